@@ -38,6 +38,12 @@
  *                           the inverted-file ANN retrieval the paper uses
  *                           (FAISS IVF-PQ of the implementation details):
  *                           IVF-Flat and IVF-PQ over the same top-k kernels
+ *   sense_kv_write, sense_kv_read, sense_kv_attention, sense_kv_compact,
+ *   sense_kv_reserve, sense_kv_fork, sense_kv_truncate
+ *                           the target model's key/value cache held in 4 bits
+ *                           in pages: its rows, attention of tokens, prompt
+ *                           chunks and draft trees over it, and what grows,
+ *                           shares, cuts it and keeps an accepted path
  *   sense_project           PCA projection + L2 normalisation of hidden
  *                           states: the query k = L2Norm(PCA(h)) of Alg. 2
  *                           and the projected datastore keys (Sec. 3.2
@@ -630,6 +636,200 @@ sense_status_t sense_ivf_search(const sense_index_t *index, const void *queries,
                                 int32_t nprobe, int64_t *out_ids, float *out_scores,
                                 int32_t *out_drafts, int32_t *out_draft_len, int64_t *out_probe,
                                 void *workspace, size_t workspace_bytes, void *stream);
+
+/* ---- The target model's key/value cache, held in 4 bits in pages: what the
+ * forward over a draft tree reads and writes (Sec. 3.2, App. tree attention),
+ * and what moves its rows when a path of the tree is accepted.
+ *
+ * A row (one token's key or value of one head, head_dim values) is held in
+ * blocks of 32 neighbours: 32 codes of 4 bits and one scale byte.  A code is
+ * sign * {0, .5, 1, 1.5, 2, 3, 4, 6}[low three bits] (bit 3: the sign), a
+ * value is code * 2^(scale - 127); scale 255 makes the whole block NaN.
+ *
+ * All arrays are the caller's DEVICE memory (no handle):
+ *   codes       uint8 [n_layers][n_pages][2][n_kv_heads][page_size][head_dim/2]
+ *               (2: keys, values); element 2i of a row in the low half of
+ *               byte i.  16-byte aligned.
+ *   scales      uint8 [n_layers][n_pages][2][n_kv_heads][head_dim/32][page_size]
+ *               16-byte aligned.
+ *   page_table  int32 [n_seqs][max_pages]: position p of sequence s is slot
+ *               p % page_size of page page_table[s][p / page_size].
+ *   seq_len     int32 [n_seqs]: positions in use.
+ *   page_refs   int32 [n_pages]: sequences that hold a page; <= 0 is free.
+ * An empty cache is page_table -1, seq_len 0, page_refs 0.
+ *   page_size 16, 32, 64 or 128; head_dim 64, 128 or 256; n_layers <= 4096;
+ *   n_kv_heads <= 1024; n_pages, n_seqs <= 2^26; max_pages * page_size <= 2^30.
+ * The table, lengths and counts are read on the device when the work runs, so
+ * captured calls replay on what the cache holds then.  Lengths are clamped to
+ * [0, max_pages * page_size] and a page id outside [0, n_pages) is no page: its
+ * positions are attended by nothing, read as 0 and not written.
+ * Calls that change a cache and calls that read what they change belong on one
+ * stream (or are ordered by events).  A page operation takes at most 4096
+ * entries. */
+typedef struct {
+    void *codes;
+    void *scales;
+    int32_t *page_table;
+    int32_t *seq_len;
+    int32_t *page_refs;
+    int32_t n_layers;
+    int32_t n_pages;
+    int32_t page_size;
+    int32_t n_kv_heads;
+    int32_t head_dim;
+    int32_t n_seqs;
+    int32_t max_pages;
+} sense_kv_cache_t;
+
+/* The sequences of a call and their rows in its tensors.  Entry i is sequence
+ * seqs[i] (i when seqs is NULL; then n <= n_seqs) with m = row_len[i] rows
+ * (max_rows when NULL; clamped to [0, max_rows]): row j of the entry is row
+ * row_start[i] + j of the tensors (i * max_rows + j when NULL) and stands for
+ * position seq_len - m + j, the last m positions of the sequence.  Rows outside
+ * [0, n_rows), positions below 0 and entries of no sequence are left out.
+ * n <= 65536, 1 <= max_rows <= 2^20; arrays are DEVICE memory. */
+typedef struct {
+    const int32_t *seqs;
+    const int32_t *row_start;
+    const int32_t *row_len;
+    int32_t n;
+    int32_t max_rows;
+    int64_t n_rows;
+} sense_kv_batch_t;
+
+/* What a page operation did for an entry (out_status, int32). */
+typedef enum SENSE_ENUM_BASE {
+    SENSE_KV_DONE = 0,
+    SENSE_KV_NO_PAGES = 1, /* too few free pages for it and those in front */
+    SENSE_KV_TOO_LONG = 2, /* beyond max_pages pages */
+    SENSE_KV_REFUSED = 3   /* see each operation; the entry changed nothing */
+} sense_kv_status_t;
+
+/* Write the rows of a batch into n_layers layers from `layer` on.  With a the
+ * largest magnitude of a block, its unit is 2^max(floor(log2 a) - 2, -127)
+ * (a = 0: 2^-127) and each value is held as the nearest code in that unit, at
+ * the even code between two and at 6 beyond 6.  A block that holds a NaN or an
+ * infinity is held as NaN.
+ *   k, v        rows of n_kv_heads x head_dim elements of dtype (F32, F16,
+ *               BF16), head h at h * head_dim; row_stride elements apart,
+ *               layer l at l * layer_stride (l = 0 is `layer`; layer_stride
+ *               is read only when n_layers > 1).  Bases and strides multiples
+ *               of 16 bytes.
+ * A sequence that is listed twice is written by its first entry.  A page that
+ * sequences share changes for all of them: sense_kv_reserve before writing
+ * gives a sequence pages of its own.
+ * Errors: INVALID_ARGUMENT, MISALIGNED, UNSUPPORTED (more workgroups than one
+ * launch holds), HIP. */
+sense_status_t sense_kv_write(const sense_kv_cache_t *cache, int32_t layer, int32_t n_layers,
+                              const void *k, const void *v, sense_dtype_t dtype,
+                              int64_t row_stride, int64_t layer_stride,
+                              const sense_kv_batch_t *batch, void *stream);
+
+/* Read the rows of a batch back as values (rounded to dtype, nearest-even;
+ * exact in F32 and BF16 up to overflow).  Arguments and errors as
+ * sense_kv_write; rows that the batch leaves out keep their contents. */
+sense_status_t sense_kv_read(const sense_kv_cache_t *cache, int32_t layer, int32_t n_layers,
+                             void *out_k, void *out_v, sense_dtype_t dtype, int64_t row_stride,
+                             int64_t layer_stride, const sense_kv_batch_t *batch, void *stream);
+
+/* Bytes of device workspace sense_kv_attention needs for n entries of up to
+ * max_rows rows.  max_kv: a bound on the sequences' lengths, 0 for the cache's
+ * capacity; pass the same value to sense_kv_attention. */
+sense_status_t sense_kv_attention_workspace_size(const sense_kv_cache_t *cache, int32_t n,
+                                                 int32_t max_rows, int32_t n_heads,
+                                                 int32_t max_kv, size_t *bytes);
+
+/* Attention of a batch's rows over the cache (their own keys and values are
+ * written first): for row j of an entry with m rows and length L, query head
+ * h and key head h / (n_heads / n_kv_heads),
+ *   out = sum_p w_p v_p / sum_p w_p,  w_p = exp(softmax_scale q . k_p)
+ * over the positions p < L that the row sees: with base = L - m,
+ *   mask NULL   p <= base + j (causal);
+ *   else        p < base, and p = base + u where
+ *               mask[i * mask_stride + j * mask_ld + u] != 0
+ * (for a draft tree the mask of sense_build_loose_trie, row_len its tree_len).
+ * A row that sees nothing becomes 0.  Positions that a row does not see do not
+ * touch it, whatever they hold.  Statistics and sums are fp32; cached values
+ * enter in q_dtype (exact in BF16; in F16 within its range), weights are
+ * rounded to q_dtype.
+ *   q, out      rows of n_heads x head_dim elements of q_dtype (F16, BF16),
+ *               head h at h * head_dim; strides in elements; bases and strides
+ *               multiples of 16 bytes.  out may be q.  Rows that the batch
+ *               leaves out keep their contents.
+ *   n_heads     a multiple of n_kv_heads, at most 4096.
+ *   mask        uint8 (DEVICE) or NULL; mask_ld >= max_rows.
+ *   softmax_scale  positive and finite.
+ *   max_kv      a bound on the lengths (0: the capacity).  Longer sequences
+ *               are attended in full all the same; the bound sizes the
+ *               workspace, and where it is small the call is one launch.
+ *   workspace   sense_kv_attention_workspace_size bytes (may be 0), 256-byte
+ *               aligned; contents not preserved.
+ * Errors: INVALID_ARGUMENT, MISALIGNED, UNSUPPORTED (more workgroups than one
+ * launch holds), WORKSPACE, HIP. */
+sense_status_t sense_kv_attention(const sense_kv_cache_t *cache, int32_t layer, const void *q,
+                                  sense_dtype_t q_dtype, int32_t n_heads, int64_t q_stride,
+                                  const sense_kv_batch_t *batch, const uint8_t *mask,
+                                  int64_t mask_ld, int64_t mask_stride, float softmax_scale,
+                                  int32_t max_kv, void *out, int64_t out_stride, void *workspace,
+                                  size_t workspace_bytes, void *stream);
+
+/* Cut sequences to lens[i] positions (lens NULL: to 0, which frees them); a
+ * shorter one stays.  Pages behind the end leave the sequence and are free
+ * when no other holds them.  Entry i is sequence seqs[i] (i when NULL).
+ * REFUSED: no such sequence, lens[i] < 0.  out_status n int32 or NULL.
+ * Errors: INVALID_ARGUMENT, MISALIGNED, HIP. */
+sense_status_t sense_kv_truncate(const sense_kv_cache_t *cache, const int32_t *seqs,
+                                 const int32_t *lens, int32_t n, int32_t *out_status,
+                                 void *stream);
+
+/* Let sequence dst[i] hold what src[i] holds, by sharing its pages.  REFUSED:
+ * no such sequence, dst[i] is not empty or was listed before, src[i] is some
+ * entry's destination.  A source may be listed many times. */
+sense_status_t sense_kv_fork(const sense_kv_cache_t *cache, const int32_t *src,
+                             const int32_t *dst, int32_t n, int32_t *out_status, void *stream);
+
+/* Bytes of device workspace sense_kv_reserve needs. */
+sense_status_t sense_kv_reserve_workspace_size(const sense_kv_cache_t *cache, int32_t n,
+                                               size_t *bytes);
+
+/* Grow sequences by counts[i] positions: free pages are given out in the order
+ * of their numbers, entries served in order.  A last page that is partly
+ * filled and shared is copied first (all layers, the filled positions), a page
+ * of the entry's own taking its place; of the entries of one call that share a
+ * page, the last holder keeps it.  New positions hold nothing in particular
+ * until they are written.  NO_PAGES: the free pages do not reach for this entry
+ * and all in front of it (then none behind it is served either).  TOO_LONG:
+ * beyond max_pages pages.  REFUSED: no such sequence, counts[i] < 0, or the
+ * sequence was listed before.
+ * Errors: INVALID_ARGUMENT, MISALIGNED, WORKSPACE, HIP. */
+sense_status_t sense_kv_reserve(const sense_kv_cache_t *cache, const int32_t *seqs,
+                                const int32_t *counts, int32_t n, int32_t *out_status,
+                                void *workspace, size_t workspace_bytes, void *stream);
+
+/* Bytes of device workspace sense_kv_compact needs. */
+sense_status_t sense_kv_compact_workspace_size(int32_t n, int32_t keep_ld, size_t *bytes);
+
+/* Keep of the last tails[i] positions of a sequence (a draft tree's nodes, in
+ * the order of sense_build_loose_trie) those of an accepted path: position
+ * base + j takes what position base + keep[j] holds, in every layer, the length
+ * becomes base + the path's, and pages behind it are released.
+ *   keep        n x keep_rows x keep_ld int32 node numbers; keep_len
+ *               n x keep_rows int32 lengths (clamped to [0, keep_ld]).  The
+ *               path is the leading run of strictly ascending numbers in
+ *               [0, tails[i]) of row pick[i] (row 0 when pick is NULL; then
+ *               keep_rows is 1).  gamma, out_accept_len and out_best of the
+ *               trie and its verification are keep, keep_len and pick.
+ *   1 <= keep_ld <= 4096.
+ * REFUSED: no such sequence or listed before, tails[i] outside [0, length],
+ * pick[i] outside [0, keep_rows), or a row would move into a page that another
+ * sequence holds too.
+ * Errors: INVALID_ARGUMENT, MISALIGNED, UNSUPPORTED (more workgroups than one
+ * launch holds), WORKSPACE, HIP. */
+sense_status_t sense_kv_compact(const sense_kv_cache_t *cache, const int32_t *seqs,
+                                const int32_t *tails, const int32_t *keep,
+                                const int32_t *keep_len, const int32_t *pick, int32_t keep_rows,
+                                int32_t keep_ld, int32_t n, int32_t *out_status, void *workspace,
+                                size_t workspace_bytes, void *stream);
 
 /* Diagnostics for benchmarks and profilers.  Which part of the path a pair
  * of timing events brackets. */

@@ -12,6 +12,7 @@
 #include <new>
 
 #include "internal.h"
+#include "kv.h"
 #include "sense.h"
 
 #define SENSE_EXPORT extern "C" __attribute__((visibility("default")))
@@ -205,6 +206,8 @@ SENSE_EXPORT const char* sense_status_string(sense_status_t s) {
     }
     return "unknown status";
 }
+
+void sense::set_last_error(const char* msg) { snprintf(g_msg, sizeof g_msg, "%s", msg); }
 
 SENSE_EXPORT const char* sense_last_error_message(void) { return g_msg; }
 

@@ -59,6 +59,16 @@ EXPORTED = (
     "sense_build_ivf_index",
     "sense_ivf_search_workspace_size",
     "sense_ivf_search",
+    "sense_kv_write",
+    "sense_kv_read",
+    "sense_kv_attention_workspace_size",
+    "sense_kv_attention",
+    "sense_kv_truncate",
+    "sense_kv_fork",
+    "sense_kv_reserve_workspace_size",
+    "sense_kv_reserve",
+    "sense_kv_compact_workspace_size",
+    "sense_kv_compact",
     "sense_set_timer_events",
     "sense_read_bandwidth_probe",
     "sense_status_string",
@@ -66,6 +76,7 @@ EXPORTED = (
 )
 SENSE_TIMER_SCAN, SENSE_TIMER_TOPK, SENSE_TIMER_VERIFY, SENSE_TIMER_SELECT = 0, 1, 2, 3
 SENSE_TIMER_TRIE, SENSE_TIMER_PROJECT, SENSE_TIMER_IVF, SENSE_TIMER_FILTER = 4, 5, 6, 7
+SENSE_KV_DONE, SENSE_KV_NO_PAGES, SENSE_KV_TOO_LONG, SENSE_KV_REFUSED = 0, 1, 2, 3
 
 
 class SenseError(RuntimeError):
@@ -160,6 +171,34 @@ class IvfDesc(ctypes.Structure):
     ]
 
 
+class KvCacheDesc(ctypes.Structure):
+    _fields_ = [
+        ("codes", ctypes.c_void_p),
+        ("scales", ctypes.c_void_p),
+        ("page_table", ctypes.c_void_p),
+        ("seq_len", ctypes.c_void_p),
+        ("page_refs", ctypes.c_void_p),
+        ("n_layers", ctypes.c_int32),
+        ("n_pages", ctypes.c_int32),
+        ("page_size", ctypes.c_int32),
+        ("n_kv_heads", ctypes.c_int32),
+        ("head_dim", ctypes.c_int32),
+        ("n_seqs", ctypes.c_int32),
+        ("max_pages", ctypes.c_int32),
+    ]
+
+
+class KvBatchDesc(ctypes.Structure):
+    _fields_ = [
+        ("seqs", ctypes.c_void_p),
+        ("row_start", ctypes.c_void_p),
+        ("row_len", ctypes.c_void_p),
+        ("n", ctypes.c_int32),
+        ("max_rows", ctypes.c_int32),
+        ("n_rows", ctypes.c_int64),
+    ]
+
+
 class GateParams(ctypes.Structure):
     _fields_ = [
         ("gamma", ctypes.c_float),
@@ -186,6 +225,7 @@ def load_library() -> ctypes.CDLL:
     P, I32, I64, SZ = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
     PP = ctypes.POINTER(ctypes.c_void_p)
     PSZ = ctypes.POINTER(ctypes.c_size_t)
+    KVC, KVB = ctypes.POINTER(KvCacheDesc), ctypes.POINTER(KvBatchDesc)
     sig = {
         "sense_build_index": [ctypes.POINTER(IndexDesc), P, PP],
         "sense_destroy_index": [P],
@@ -211,6 +251,17 @@ def load_library() -> ctypes.CDLL:
         "sense_ivf_search": [P, P, ctypes.c_int, I32, I32, I32, P, P, P, P, P, P, SZ, P],
         "sense_project": [ctypes.POINTER(ProjDesc), P, ctypes.c_int, I64, I64, P, ctypes.c_int,
                           I64, P, SZ, P],
+        "sense_kv_write": [KVC, I32, I32, P, P, ctypes.c_int, I64, I64, KVB, P],
+        "sense_kv_read": [KVC, I32, I32, P, P, ctypes.c_int, I64, I64, KVB, P],
+        "sense_kv_attention_workspace_size": [KVC, I32, I32, I32, I32, PSZ],
+        "sense_kv_attention": [KVC, I32, P, ctypes.c_int, I32, I64, KVB, P, I64, I64,
+                               ctypes.c_float, I32, P, I64, P, SZ, P],
+        "sense_kv_truncate": [KVC, P, P, I32, P, P],
+        "sense_kv_fork": [KVC, P, P, I32, P, P],
+        "sense_kv_reserve_workspace_size": [KVC, I32, PSZ],
+        "sense_kv_reserve": [KVC, P, P, I32, P, P, SZ, P],
+        "sense_kv_compact_workspace_size": [I32, I32, PSZ],
+        "sense_kv_compact": [KVC, P, P, P, P, P, I32, I32, I32, P, P, SZ, P],
         "sense_soft_gate_verify_tree_workspace_size": [I32, I32, I32, I32, PSZ],
         "sense_soft_gate_verify_tree": [P, ctypes.c_int, I64, P, P, P, P, I32, I32, I32, I32,
                                         ctypes.POINTER(GateParams), P, P, P, P, P, P, SZ, P],
@@ -866,3 +917,328 @@ def sense_ivf_search(index: IvfIndex, queries: torch.Tensor, k: int, nprobe: int
                                 _dev_ptr(workspace, "workspace"), workspace.numel(),
                                 _stream_handle(stream)), "sense_ivf_search")
     return (ids, sc, dr, dl, probe) if want_probe else (ids, sc, dr, dl)
+
+
+# ------------------------------------------- the 4-bit paged key/value cache
+#
+# A cache is a dict of GPU tensors (all of one device):
+#   codes       uint8 [layers, pages, 2, kv_heads, page_size, head_dim / 2]
+#   scales      uint8 [layers, pages, 2, kv_heads, head_dim / 32, page_size]
+#   page_table  int32 [n_seqs, max_pages]    (-1: no page)
+#   seq_len     int32 [n_seqs]
+#   page_refs   int32 [pages]                (0: free)
+
+
+def sense_build_kv_cache(n_layers: int, n_pages: int, page_size: int, n_kv_heads: int,
+                         head_dim: int, n_seqs: int, max_pages: int,
+                         device: torch.device | str = "cuda") -> dict:
+    """An empty cache (the dict described above) of ``n_pages`` pages for
+    ``n_seqs`` sequences of up to ``max_pages`` pages each."""
+    u8, i32 = dict(dtype=torch.uint8, device=device), dict(dtype=torch.int32, device=device)
+    cache = {
+        "codes": torch.zeros((n_layers, n_pages, 2, n_kv_heads, page_size, head_dim // 2), **u8),
+        "scales": torch.zeros((n_layers, n_pages, 2, n_kv_heads, head_dim // 32, page_size), **u8),
+        "page_table": torch.full((n_seqs, max_pages), -1, **i32),
+        "seq_len": torch.zeros(n_seqs, **i32),
+        "page_refs": torch.zeros(n_pages, **i32),
+    }
+    _kv_desc(cache)
+    if page_size not in (16, 32, 64, 128) or head_dim not in (64, 128, 256):
+        raise ValueError("page_size is 16, 32, 64 or 128 and head_dim 64, 128 or 256")
+    return cache
+
+
+def _kv_desc(cache: dict) -> KvCacheDesc:
+    codes, scales = cache["codes"], cache["scales"]
+    table, lens, refs = cache["page_table"], cache["seq_len"], cache["page_refs"]
+    if codes.dim() != 6 or scales.dim() != 6 or table.dim() != 2:
+        raise ValueError("codes and scales must have 6 dimensions, page_table 2")
+    layers, pages, two, heads, page, half = codes.shape
+    if two != 2 or tuple(scales.shape) != (layers, pages, 2, heads, half // 16, page):
+        raise ValueError("codes are [layers, pages, 2, heads, page, d/2] and scales "
+                         "[layers, pages, 2, heads, d/32, page]")
+    if lens.shape != (table.shape[0],) or refs.shape != (pages,):
+        raise ValueError("seq_len has an entry a row of page_table, page_refs one a page")
+    dev = codes.device
+    for t, dtype, name in ((codes, torch.uint8, "codes"), (scales, torch.uint8, "scales"),
+                           (table, torch.int32, "page_table"), (lens, torch.int32, "seq_len"),
+                           (refs, torch.int32, "page_refs")):
+        if t.dtype != dtype or not t.is_contiguous() or t.device != dev:
+            raise ValueError(f"{name} must be a contiguous {dtype} tensor on {dev}")
+    return KvCacheDesc(codes=_dev_ptr(codes, "codes"), scales=scales.data_ptr(),
+                       page_table=table.data_ptr(), seq_len=lens.data_ptr(),
+                       page_refs=refs.data_ptr(), n_layers=layers, n_pages=pages, page_size=page,
+                       n_kv_heads=heads, head_dim=2 * half, n_seqs=table.shape[0],
+                       max_pages=table.shape[1])
+
+
+class _KvCall:
+    """A call on a cache: its device is made current and, where a stream is
+    named, that stream too, so that what is allocated inside belongs to it."""
+
+    def __init__(self, cache: dict, stream):
+        dev = cache["codes"].device
+        self.contexts = []
+        if dev.index != torch.cuda.current_device():
+            self.contexts.append(torch.cuda.device(dev))
+        if stream is not None:
+            if not isinstance(stream, torch.cuda.Stream):
+                stream = torch.cuda.ExternalStream(int(stream), device=dev)
+            self.contexts.append(torch.cuda.stream(stream))
+
+    def __enter__(self):
+        for c in self.contexts:
+            c.__enter__()
+        return _stream_handle(None)
+
+    def __exit__(self, *exc):
+        for c in reversed(self.contexts):
+            c.__exit__(*exc)
+
+
+def _kv_scratch(cache: dict, workspace: torch.Tensor | None, size_call: str, *args):
+    """The caller's workspace, or one of the size that ``size_call`` names."""
+    if workspace is None:
+        size = ctypes.c_size_t()
+        _check(getattr(load_library(), size_call)(*args, ctypes.byref(size)), size_call)
+        workspace = torch.empty(max(size.value, 1), dtype=torch.uint8,
+                                device=cache["codes"].device)
+    if workspace.dtype != torch.uint8 or not workspace.is_contiguous() \
+            or workspace.device != cache["codes"].device:
+        raise ValueError("workspace must be a contiguous uint8 tensor on the cache's device")
+    return workspace
+
+
+def _kv_ints(t: torch.Tensor | None, n: int | None, cache: dict, name: str):
+    """The address of an int32 tensor of n entries on the cache's device."""
+    if t is None:
+        return None
+    if (t.dtype != torch.int32 or not t.is_contiguous() or t.device != cache["codes"].device
+            or (n is not None and t.numel() != n)):
+        raise ValueError(f"{name} must be a contiguous int32 tensor"
+                         f"{'' if n is None else f' of {n} entries'} on the cache's device")
+    return t.data_ptr()
+
+
+def _kv_batch(cache: dict, lead: tuple, seqs, row_start, row_len, max_rows) -> KvBatchDesc:
+    """Entries and rows of a call on tensors whose leading dimensions are
+    ``lead``: (n, max_rows), or (rows,) with row_start, row_len and max_rows."""
+    if len(lead) == 2:
+        n, m = lead
+        if row_start is not None or (max_rows is not None and max_rows != m):
+            raise ValueError("row_start and max_rows belong to tensors of one row dimension")
+    else:
+        if row_start is None or row_len is None or max_rows is None:
+            raise ValueError("tensors of one row dimension need row_start, row_len and max_rows")
+        n, m = row_start.numel(), max_rows
+    return KvBatchDesc(seqs=_kv_ints(seqs, n, cache, "seqs"),
+                       row_start=_kv_ints(row_start, n, cache, "row_start"),
+                       row_len=_kv_ints(row_len, n, cache, "row_len"), n=n, max_rows=m,
+                       n_rows=n * m if len(lead) == 2 else lead[0])
+
+
+def _kv_row_stride(t: torch.Tensor, first: int, name: str) -> int:
+    """Elements between rows of t, whose row dimensions begin at ``first`` and
+    whose last two are heads and head_dim."""
+    d = t.shape[-1]
+    if t.stride(-1) != 1 or (t.shape[-2] > 1 and t.stride(-2) != d):
+        raise ValueError(f"{name}: heads and head_dim must be contiguous")
+    if t.dim() - first == 3:
+        return t.stride(first) if t.shape[first] > 1 else t.shape[-2] * d
+    n, m = t.shape[first], t.shape[first + 1]
+    row = (t.stride(first + 1) if m > 1 else t.stride(first) if n > 1 else t.shape[-2] * d)
+    if n > 1 and m > 0 and t.stride(first) != m * row:
+        raise ValueError(f"{name}: entries must follow one another (stride m * row stride)")
+    return row
+
+
+def _kv_rows(fn: str, cache: dict, layer: int, k: torch.Tensor, v: torch.Tensor, seqs, row_start,
+             row_len, max_rows, stream) -> None:
+    desc = _kv_desc(cache)
+    if k.shape != v.shape or k.dtype != v.dtype or k.dtype not in _TORCH_DTYPE:
+        raise ValueError("k and v must be float32/float16/bfloat16 tensors of one shape and type")
+    if tuple(k.shape[-2:]) != (desc.n_kv_heads, desc.head_dim):
+        raise ValueError(f"k and v rows must be {desc.n_kv_heads} x {desc.head_dim}")
+    dev = cache["codes"].device
+    if k.device != dev or v.device != dev:
+        raise ValueError(f"k and v must be on {dev}")
+    layers = 1
+    first = 0
+    if k.dim() == 5 or (k.dim() == 4 and row_start is not None):
+        layers, first = k.shape[0], 1
+    if k.dim() - first not in (3, 4):
+        raise ValueError("k and v are [n, max_rows, heads, d] or [rows, heads, d], either with a "
+                         "dimension of layers in front")
+    row, layer_stride = _kv_row_stride(k, first, "k"), k.stride(0) if first else 0
+    if _kv_row_stride(v, first, "v") != row or (layers > 1 and v.stride(0) != layer_stride):
+        raise ValueError("k and v must have the same strides")
+    batch = _kv_batch(cache, tuple(k.shape[first:-2]), seqs, row_start, row_len, max_rows)
+    if batch.n == 0 or batch.max_rows == 0 or layers == 0:
+        return
+    with _KvCall(cache, stream) as st:
+        _check(getattr(load_library(), fn)(
+            ctypes.byref(desc), layer, layers, k.data_ptr(), v.data_ptr(), _TORCH_DTYPE[k.dtype],
+            row, layer_stride, ctypes.byref(batch), st), fn)
+
+
+def sense_kv_write(cache: dict, layer: int, k: torch.Tensor, v: torch.Tensor,
+                   seqs: torch.Tensor | None = None, row_start: torch.Tensor | None = None,
+                   row_len: torch.Tensor | None = None, max_rows: int | None = None,
+                   stream=None) -> None:
+    """Quantise rows into the last positions of sequences.
+
+    ``k``, ``v``: [n, max_rows, kv_heads, d] (entry i's first row_len[i] rows,
+    all without row_len), or [rows, kv_heads, d] with ``row_start``,
+    ``row_len`` [n] and ``max_rows``; a dimension of layers in front writes
+    that many layers from ``layer`` on.  Entry i is sequence ``seqs[i]`` (i
+    without seqs); its m rows become positions seq_len - m .. seq_len - 1."""
+    _kv_rows("sense_kv_write", cache, layer, k, v, seqs, row_start, row_len, max_rows, stream)
+
+
+def sense_kv_read(cache: dict, layer: int, out_k: torch.Tensor, out_v: torch.Tensor,
+                  seqs: torch.Tensor | None = None, row_start: torch.Tensor | None = None,
+                  row_len: torch.Tensor | None = None, max_rows: int | None = None, stream=None):
+    """The values of the last positions of sequences, into ``out_k`` and
+    ``out_v`` (shaped as sense_kv_write's rows); returns them."""
+    _kv_rows("sense_kv_read", cache, layer, out_k, out_v, seqs, row_start, row_len, max_rows,
+             stream)
+    return out_k, out_v
+
+
+def sense_kv_attention_workspace_size(cache: dict, n: int, max_rows: int, n_heads: int,
+                                      max_kv: int = 0) -> int:
+    size = ctypes.c_size_t()
+    _check(load_library().sense_kv_attention_workspace_size(
+        ctypes.byref(_kv_desc(cache)), n, max_rows, n_heads, max_kv, ctypes.byref(size)),
+        "sense_kv_attention_workspace_size")
+    return size.value
+
+
+def sense_kv_attention(cache: dict, layer: int, q: torch.Tensor, mask: torch.Tensor | None = None,
+                       seqs: torch.Tensor | None = None, row_start: torch.Tensor | None = None,
+                       row_len: torch.Tensor | None = None, max_rows: int | None = None,
+                       softmax_scale: float | None = None, max_kv: int = 0,
+                       workspace: torch.Tensor | None = None, out: torch.Tensor | None = None,
+                       stream=None) -> torch.Tensor:
+    """Attention of rows over the cache (their keys and values written first).
+
+    ``q``: [n, max_rows, heads, d] or [rows, heads, d] (float16/bfloat16), its
+    rows given as in sense_kv_write.  Row j of an entry with m rows sees the
+    first seq_len - m + j + 1 positions, or with ``mask`` (uint8 or bool
+    [n, nodes, nodes], nodes >= max_rows: sense_build_loose_trie's) all
+    positions in front of the entry's rows and those rows u that
+    mask[i, j, u] names.  ``max_kv`` bounds the sequences' lengths (0: the
+    capacity); ``softmax_scale`` is d**-0.5 by default.  Returns ``out``
+    (like q; rows that belong to no entry keep what they hold)."""
+    desc = _kv_desc(cache)
+    dev = cache["codes"].device
+    if q.dim() not in (3, 4) or q.dtype not in (torch.float16, torch.bfloat16) or q.device != dev:
+        raise ValueError(f"q must be a 3-D or 4-D float16/bfloat16 tensor on {dev}")
+    if q.shape[-1] != desc.head_dim:
+        raise ValueError(f"q has {q.shape[-1]} values a head, the cache {desc.head_dim}")
+    batch = _kv_batch(cache, tuple(q.shape[:-2]), seqs, row_start, row_len, max_rows)
+    if out is not None and (out.shape != q.shape or out.dtype != q.dtype or out.device != dev):
+        raise ValueError("out must have q's shape, type and device")
+    ld = step = 0
+    if mask is not None:
+        if mask.dtype not in (torch.uint8, torch.bool) or mask.dim() != 3 or mask.device != dev \
+                or mask.shape[0] != batch.n or min(mask.shape[1:]) < batch.max_rows \
+                or mask.stride(2) != 1:
+            raise ValueError("mask must be uint8 or bool [n, nodes, nodes] with nodes >= max_rows "
+                             "and contiguous rows")
+        ld = mask.stride(1) if mask.shape[1] > 1 else mask.shape[2]
+        step = mask.stride(0)
+    heads = q.shape[-2]
+    with _KvCall(cache, stream) as st:
+        if out is None:
+            out = torch.empty(q.shape, dtype=q.dtype, device=dev)
+        if batch.n == 0 or batch.max_rows == 0:
+            return out
+        workspace = _kv_scratch(cache, workspace, "sense_kv_attention_workspace_size",
+                                ctypes.byref(desc), batch.n, batch.max_rows, heads, max_kv)
+        _check(load_library().sense_kv_attention(
+            ctypes.byref(desc), layer, q.data_ptr(), _TORCH_DTYPE[q.dtype], heads,
+            _kv_row_stride(q, 0, "q"), ctypes.byref(batch),
+            None if mask is None else mask.data_ptr(), ld, step,
+            q.shape[-1] ** -0.5 if softmax_scale is None else softmax_scale, max_kv,
+            out.data_ptr(), _kv_row_stride(out, 0, "out"), workspace.data_ptr(),
+            workspace.numel(), st), "sense_kv_attention")
+    return out
+
+
+def _kv_status(cache: dict, n: int) -> torch.Tensor:
+    return torch.empty(n, dtype=torch.int32, device=cache["codes"].device)
+
+
+def sense_kv_truncate(cache: dict, lens: torch.Tensor | None = None,
+                      seqs: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """Cut sequences ``seqs`` (0, 1, ... without it) to ``lens`` positions (0
+    without it: the sequences are freed); returns an int32 status each."""
+    desc = _kv_desc(cache)
+    n = (seqs.numel() if seqs is not None else lens.numel() if lens is not None else desc.n_seqs)
+    with _KvCall(cache, stream) as st:
+        status = _kv_status(cache, n)
+        _check(load_library().sense_kv_truncate(
+            ctypes.byref(desc), _kv_ints(seqs, n, cache, "seqs"),
+            _kv_ints(lens, n, cache, "lens"), n, status.data_ptr(), st), "sense_kv_truncate")
+    return status
+
+
+def sense_kv_fork(cache: dict, src: torch.Tensor, dst: torch.Tensor, stream=None) -> torch.Tensor:
+    """Let the empty sequences ``dst`` share what ``src`` hold; returns an
+    int32 status each."""
+    desc = _kv_desc(cache)
+    n = src.numel()
+    with _KvCall(cache, stream) as st:
+        status = _kv_status(cache, n)
+        _check(load_library().sense_kv_fork(
+            ctypes.byref(desc), _kv_ints(src, n, cache, "src"), _kv_ints(dst, n, cache, "dst"), n,
+            status.data_ptr(), st), "sense_kv_fork")
+    return status
+
+
+def sense_kv_reserve(cache: dict, counts: torch.Tensor, seqs: torch.Tensor | None = None,
+                     workspace: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """Grow sequences ``seqs`` (0, 1, ... without it) by ``counts`` positions,
+    copying a shared last page first; returns an int32 status each."""
+    desc = _kv_desc(cache)
+    n = counts.numel()
+    with _KvCall(cache, stream) as st:
+        status = _kv_status(cache, n)
+        workspace = _kv_scratch(cache, workspace, "sense_kv_reserve_workspace_size",
+                                ctypes.byref(desc), n)
+        _check(load_library().sense_kv_reserve(
+            ctypes.byref(desc), _kv_ints(seqs, n, cache, "seqs"),
+            _kv_ints(counts, n, cache, "counts"), n, status.data_ptr(),
+            workspace.data_ptr(), workspace.numel(), st), "sense_kv_reserve")
+    return status
+
+
+def sense_kv_compact(cache: dict, tails: torch.Tensor, keep: torch.Tensor,
+                     keep_len: torch.Tensor, pick: torch.Tensor | None = None,
+                     seqs: torch.Tensor | None = None, workspace: torch.Tensor | None = None,
+                     stream=None) -> torch.Tensor:
+    """Keep an accepted path of each sequence's last ``tails`` positions.
+
+    ``keep`` [n * rows, ld] (or [n, rows, ld]) int32 node numbers and
+    ``keep_len`` [n * rows]; ``pick`` [n] names each entry's row (needed when
+    rows > 1): gamma, accept_len and best of the trie and its verification.
+    Returns an int32 status each."""
+    desc = _kv_desc(cache)
+    n = tails.numel()
+    rows = keep.numel() // max(1, n * keep.shape[-1])
+    if n * rows * keep.shape[-1] != keep.numel() or (n and rows < 1):
+        raise ValueError("keep must be [n, ld] or [n * rows, ld]")
+    if rows > 1 and pick is None:
+        raise ValueError("pick must name the row of each entry")
+    with _KvCall(cache, stream) as st:
+        status = _kv_status(cache, n)
+        workspace = _kv_scratch(cache, workspace, "sense_kv_compact_workspace_size", n,
+                                keep.shape[-1])
+        _check(load_library().sense_kv_compact(
+            ctypes.byref(desc), _kv_ints(seqs, n, cache, "seqs"),
+            _kv_ints(tails, n, cache, "tails"), _kv_ints(keep, None, cache, "keep"),
+            _kv_ints(keep_len, n * rows, cache, "keep_len"), _kv_ints(pick, n, cache, "pick"),
+            max(rows, 1), keep.shape[-1], n, status.data_ptr(),
+            workspace.data_ptr(), workspace.numel(), st), "sense_kv_compact")
+    return status
