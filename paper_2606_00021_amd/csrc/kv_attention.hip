@@ -4,8 +4,8 @@
 //   positions p that row j sees
 //
 // in one pass over the cache: the running maximum m and the sums of
-// exp(s - m) and exp(s - m) v are kept in fp32, rescaled only when a score
-// passes m by more than 2^8 (see kSlack).
+// exp(s - m) and exp(s - m) v are kept in fp32, rescaled only when a weight
+// passes 2^8.
 //
 // A unit is the rows of one entry that share a key head: new tokens times
 // query heads per key head, in tiles of 16 MT rows.  A unit's keys are cut
@@ -22,15 +22,19 @@
 // in the lane, and the scores of two key tiles are, as they lie, the B operand
 // of the second product.  Contractions may take dims and keys in any order:
 //   - lane group g = lane >> 4 takes dims [g d/4, (g+1) d/4) of a key, d/8
-//     bytes in one load, the tiles' key rows being 8 (m >> 2) + 4 t + (m & 3);
-//   - in the second product lane (m, g) has keys 8g .. 8g+7 and dims
-//     [m d/16, (m+1) d/16): whole bytes of codes, of one scale a key.  Codes
-//     of two keys are widened by v_cvt_scalef32_pk and exchanged in pairs by
-//     v_perm, so nothing passes through LDS.
+//     bytes in one load;
+//   - in the second product lane (m, g) has keys 4g .. 4g+3 of both key tiles
+//     and dims [m d/16, (m+1) d/16): whole bytes of codes, of one scale a key.
+//     Codes of two keys are widened by v_cvt_scalef32_pk and exchanged in
+//     pairs by v_perm, so nothing passes through LDS.
+// A key tile lies in one page, so every load has a base that is the same for
+// the wave and an offset that is the same for all steps.
 // 4-bit values times their scales are exact in bf16, and in f16 where they lie
 // in its range.  Probabilities are rounded to the query's type (nearest);
 // their sum is taken of the rounded ones, by a product with ones, so that the
 // weights that are used add up to 1.
+#include <type_traits>
+
 #include "internal.h"
 #include "kv.h"
 
@@ -41,7 +45,6 @@ constexpr int kThreads = 256;
 constexpr int kWaves = 4;
 constexpr int kStep = 32;              // keys of a wave's step
 constexpr int kTile = kStep * kWaves;  // keys of a workgroup's step
-constexpr float kSlack = 8.f;          // scores may pass the reference by 2^8
 // A unit is not cut below this many keys: a shorter run costs more in joining
 // than its parallelism gains.
 constexpr int kMinRun = 256;
@@ -49,10 +52,16 @@ constexpr int kMinRun = 256;
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+
+// The page table is not written while these kernels run: scalar loads.
+typedef const __attribute__((address_space(4))) int32_t* ScalarInts;
+
+constexpr int kXcdRun = 8;             // items of a run (tiles of more than 32 rows)
 
 struct Args {
     KvCache c;
@@ -82,9 +91,9 @@ __device__ __forceinline__ int64_t wave_sum64(int64_t v) {
 
 // The items of the entries, in order, computed by every wave for itself from
 // the entries' lengths.  entry < 0: the entry that this workgroup's item
-// belongs to; else that entry.  Items go to the XCDs in runs (workgroups are
-// dealt to the 8 XCDs in turn): tiles of one unit, which read the same keys,
-// then share an L2.
+// belongs to; else that entry.  Workgroups are dealt to the 8 XCDs in turn;
+// items go to them in short runs, so that tiles which read the same keys share
+// an L2 and every XCD still has its part of each entry.
 template <int ROWS>
 __device__ __forceinline__ Plan plan(const Args& g, int entry) {
     const int lane = threadIdx.x & 63;
@@ -103,7 +112,7 @@ __device__ __forceinline__ Plan plan(const Args& g, int entry) {
     int64_t run64 = g.target ? (work + g.target - 1) / g.target : 1 << 24;
     if (run64 < kMinRun / kTile) run64 = kMinRun / kTile;
     Plan p;
-    p.run = (int)(run64 < (1 << 24) ? run64 : (1 << 24));
+    p.run = __builtin_amdgcn_readfirstlane((int)(run64 < (1 << 24) ? run64 : (1 << 24)));
     int mine = 0;
     for (int e = e0; e < e1; ++e) {
         const int s = kv_seq(g.c, g.b.seqs, e);
@@ -119,9 +128,9 @@ __device__ __forceinline__ Plan plan(const Args& g, int entry) {
         const int o = __shfl_up(upto, s);
         if (lane >= s) upto += o;
     }
-    const int total = __shfl(upto, 63), share = (total + 7) >> 3;
+    constexpr int kRun = ROWS <= 32 ? 1 : kXcdRun;
     const int idx = (int)(blockIdx.x >> 3);
-    const int item = idx < share ? (int)(blockIdx.x & 7) * share + idx : total;
+    const int item = ((idx / kRun) * 8 + (int)(blockIdx.x & 7)) * kRun + idx % kRun;
     p.item = item;
     const bool owner = entry < 0 ? (item >= upto - mine && item < upto)
                                  : (entry >= e0 && entry < e1);
@@ -133,8 +142,8 @@ __device__ __forceinline__ Plan plan(const Args& g, int entry) {
     if (!who) return p;
     const int src = __builtin_ctzll(who);
     // Walked by every lane alike: the owner's chunk.
-    int at = __shfl(upto - mine, src);
-    const int c0 = __shfl(e0, src), c1 = __shfl(e1, src);
+    int at = __builtin_amdgcn_readlane(upto - mine, src);
+    const int c0 = __builtin_amdgcn_readlane(e0, src), c1 = __builtin_amdgcn_readlane(e1, src);
     for (int e = c0; e < c1; ++e) {
         const int s = kv_seq(g.c, g.b.seqs, e);
         if (s < 0) continue;
@@ -195,6 +204,14 @@ __device__ __forceinline__ uint32_t pack(float a, float b) {
         return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2));
 }
 
+// Whether a weight of the lane's row, in any of its four lanes, is beyond
+// `limit`.  A row takes a new reference only then, so that its result does not
+// depend on the rows that it shares a wave with.
+__device__ __forceinline__ bool row_over(uint32_t most, uint32_t limit) {
+    const uint64_t over = __ballot(most > limit);
+    return (over | over >> 16 | over >> 32 | over >> 48) >> (threadIdx.x & 15) & 1;
+}
+
 __device__ __forceinline__ float unit_of(uint32_t byte) {
     return __builtin_bit_cast(float, byte << 23);
 }
@@ -203,14 +220,19 @@ __device__ __forceinline__ float unit_of(uint32_t byte) {
 template <int D>
 struct Step {
     uint32_t k[2][D / 32];              // d/8 bytes of a key, per key tile
-    uint32_t ks[2];                     // its scales: one byte, two of 256 dims
-    uint32_t v[8 * D / 128 + (D == 64 ? 4 : 0)];   // d/32 bytes of each of 8 keys
-    uint32_t vs[2];                     // 8 scale bytes
-    int bad;                            // halves of the step without a page
+    uint32_t ks[2][D == 256 ? 2 : 1];   // its scale bytes
+    uint32_t v[2][4][D == 256 ? 2 : 1]; // d/32 bytes of four keys, per key tile
+    uint32_t vs[2];                     // their scale bytes
+};
+
+// Pages of a step's two key tiles; bit t of `bad`: tile t has none.
+struct Pages {
+    int id[2];
+    int bad;
 };
 
 template <int D, bool F16, int MT>
-__global__ __launch_bounds__(kThreads) void kv_attention_kernel(Args g) {
+__global__ __launch_bounds__(kThreads, MT * D > 128 ? 2 : (MT == 2 ? 3 : 4)) void kv_few_kernel(Args g) {
     constexpr int kRows = 16 * MT;
     constexpr int kKs = D / 32;         // matrix steps of the first product
     constexpr int DV = D / 16;          // dims of a lane in the second
@@ -237,7 +259,6 @@ __global__ __launch_bounds__(kThreads) void kv_attention_kernel(Args g) {
 
     // Rows of the lane's column: token and whether it exists.
     int tok[MT];
-    int64_t qrow[MT];
     u32x4 qf[MT][kKs];
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
@@ -245,7 +266,6 @@ __global__ __launch_bounds__(kThreads) void kv_attention_kernel(Args g) {
         tok[mt] = r / g.group;
         const int64_t row = start + tok[mt];
         const bool on = tok[mt] < p.rows && row >= 0 && row < g.b.n_rows;
-        qrow[mt] = on ? row : -1;
         const u32x4* src = (const u32x4*)((const uint16_t*)g.a.q + (on ? row : 0) * g.a.q_stride +
                                           ((int64_t)head * g.group + r % g.group) * D +
                                           grp * (D / 4));
@@ -267,137 +287,163 @@ __global__ __launch_bounds__(kThreads) void kv_attention_kernel(Args g) {
 
     f32x4 o[DV][MT];
     f32x4 lsum[MT];
-    float ref[MT], neg[MT];             // reference of the exponents, and its negative or 0
-    constexpr float kLift = F16 ? 7.f : 0.f;    // f16: probabilities up to 2^15, not 2^8
+    f32x4 hit[MT];                      // NaN values that a row sees, for its dims
+    float ref[MT], neg[MT];             // reference of the exponents; kLift - it, or infinity
+    constexpr float kLift = F16 ? 7.f : 0.f;    // f16: weights up to 2^15, not 2^8
+    constexpr uint32_t kMostBits = (uint32_t)(127 + (F16 ? 15 : 8)) << 23;
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
 #pragma unroll
         for (int t = 0; t < DV; ++t) o[t][mt] = f32x4{0, 0, 0, 0};
         lsum[mt] = f32x4{0, 0, 0, 0};
+        hit[mt] = f32x4{0, 0, 0, 0};
         ref[mt] = -INFINITY;
-        neg[mt] = kLift;
+        neg[mt] = INFINITY;
     }
     const float cs = g.a.scale * 1.4426950408889634f;
     const uint32_t one = F16 ? 0x3C003C00u : 0x3F803F80u;
     const u32x4 ones = {one, one, one, one};
 
-    const int32_t* table = g.c.page_table + (int64_t)p.seq * g.c.max_pages;
+    const ScalarInts table =
+        (ScalarInts)(uintptr_t)(g.c.page_table + (int64_t)p.seq * g.c.max_pages);
     const int lg = g.c.lg_page, slot_mask = g.c.page() - 1;
     const int64_t page_rows = (int64_t)2 * g.c.heads << lg;
     const int64_t k_rows = g.c.rows_before(g.a.layer, 0, 0, head);
-    const int64_t v_rows = g.c.rows_before(g.a.layer, 0, 1, head);
+    const int64_t v_rows = k_rows + ((int64_t)g.c.heads << lg);
+    const uint32_t kc_at = col * (D / 2) + grp * (D / 8);
+    const uint32_t ks_at = ((D == 64 ? grp >> 1 : (D == 128 ? grp : 2 * grp)) << lg) + col;
+    const uint32_t vc_at = 4 * grp * (D / 2) + col * (D / 32);
+    const uint32_t vs_at = ((col * DV / 32) << lg) + 4 * grp;
 
-    auto load = [&](Step<D>& f, int key) {
-        // Pages of the step's halves (one page where pages hold 32 or more).
-        int id0 = table[key >> lg];
-        int id1 = key + 16 < p.len ? table[(key + 16) >> lg] : -1;
-        f.bad = (kv_page_ok(g.c, id0) ? 0 : 1) | (kv_page_ok(g.c, id1) ? 0 : 2);
-        id0 = f.bad & 1 ? 0 : id0;
-        id1 = f.bad & 2 ? 0 : id1;
-        const int kin = 8 * (col >> 2) + (col & 3);         // + 4 t
-        const int64_t kpage = (kin >= 16 ? id1 : id0) * page_rows + k_rows;
-        const int kslot = (key + kin) & slot_mask;
-        const uint8_t* kc = g.c.codes + (kpage + kslot) * (D / 2) + grp * (D / 8);
-        const uint8_t* ksc = g.c.scales + kpage * (D / 32) + kslot;
+    auto pages = [&](int key) {
+        Pages f;
+        f.id[0] = table[key >> lg];
+        f.id[1] = key + 16 < p.len ? table[(key + 16) >> lg] : -1;
+        return f;
+    };
+    auto load = [&](Step<D>& f, Pages& ids, int key) {
+        ids.bad = 0;
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-            const uint8_t* at = kc + t * 4 * (D / 2);
-#pragma unroll
-            for (int w = 0; w < D / 32; ++w) f.k[t][w] = ((const uint32_t*)at)[w];
-            if constexpr (D == 256) {
-                f.ks[t] = ksc[4 * t + ((2 * grp) << lg)] | ksc[4 * t + ((2 * grp + 1) << lg)] << 8;
-            } else {
-                f.ks[t] = ksc[4 * t + ((D == 64 ? grp >> 1 : grp) << lg)];
+            int id = ids.id[t];
+            if (!kv_page_ok(g.c, id)) {
+                ids.bad |= 1 << t;
+                id = 0;
             }
-        }
-        const int64_t vpage = (grp >= 2 ? id1 : id0) * page_rows + v_rows;
-        const int vslot = (key + 8 * grp) & slot_mask;
-        const uint8_t* vc = g.c.codes + (vpage + vslot) * (D / 2) + col * (D / 32);
-        const uint32_t* vsc = (const uint32_t*)(g.c.scales + vpage * (D / 32) + vslot +
-                                                (((col * DV) / 32) << lg));
+            const int slot = (key + 16 * t) & slot_mask;
+            const int64_t kr = id * page_rows + k_rows, vr = id * page_rows + v_rows;
+            const uint8_t* kc = g.c.codes + (kr + slot) * (D / 2);
+            const uint8_t* vc = g.c.codes + (vr + slot) * (D / 2);
+            const uint8_t* ks = g.c.scales + kr * (D / 32) + slot;
+            const uint8_t* vs = g.c.scales + vr * (D / 32) + slot;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            if constexpr (D == 64) {
-                f.v[i] = *(const uint16_t*)(vc + i * (D / 2));
-            } else {
+            for (int w = 0; w < D / 32; ++w) f.k[t][w] = ((const uint32_t*)(kc + kc_at))[w];
 #pragma unroll
-                for (int w = 0; w < D / 128; ++w)
-                    f.v[i * (D / 128) + w] = ((const uint32_t*)(vc + i * (D / 2)))[w];
+            for (int w = 0; w < (D == 256 ? 2 : 1); ++w) f.ks[t][w] = (ks + (w << lg))[ks_at];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if constexpr (D == 64) {
+                    f.v[t][i][0] = *(const uint16_t*)(vc + vc_at + i * (D / 2));
+                } else {
+#pragma unroll
+                    for (int w = 0; w < D / 128; ++w)
+                        f.v[t][i][w] = ((const uint32_t*)(vc + vc_at + i * (D / 2)))[w];
+                }
             }
+            f.vs[t] = *(const uint32_t*)(vs + vs_at);
         }
-        f.vs[0] = vsc[0];
-        f.vs[1] = vsc[1];
     };
 
-    auto compute = [&](Step<D>& f, int key) {
+    // One step of 32 keys.  MASKED: some row does not see some key of it.
+    auto compute = [&](const Step<D>& f, int bad, int key, auto masked) {
+        constexpr bool kMasked = decltype(masked)::value;
         // S^T: two tiles of 16 keys.
-        u32x4 kf[2][kKs];
+        f32x4 s[MT][2];
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
+        for (int q = 0; q < kKs; ++q) {
+            u32x4 kf[2];
 #pragma unroll
-            for (int s = 0; s < kKs; ++s)
-                kf[t][s] = widen8<F16>(
-                    f.k[t][s], unit_of(D == 256 ? (f.ks[t] >> (s >= 4 ? 8 : 0)) & 0xFFu : f.ks[t]));
-        const bool plain = key + kStep <= full && f.bad == 0;
-        uint32_t vis[MT];               // bit 4t + r: the row sees the key (masked steps)
-        u32x4 pf[MT];
+            for (int t = 0; t < 2; ++t)
+                kf[t] = widen8<F16>(f.k[t][q], unit_of(f.ks[t][D == 256 ? q >> 2 : 0]));
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) {
-            f32x4 s[2];
+            for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                s[t] = f32x4{0, 0, 0, 0};
+                for (int t = 0; t < 2; ++t)
+                    s[mt][t] = mfma<F16>(kf[t], qf[mt][q], q ? s[mt][t] : f32x4{0, 0, 0, 0});
+        }
+        uint32_t vis[MT] = {};          // bit 4t + r: the row sees key 4 grp + r of tile t
+        if constexpr (kMasked) {
 #pragma unroll
-                for (int q = 0; q < kKs; ++q) s[t] = mfma<F16>(kf[t][q], qf[mt][q], s[t]);
-            }
-            if (!plain) {
-                uint32_t bits = 0;
+            for (int mt = 0; mt < MT; ++mt) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    const int pos = key + 8 * grp + e;
-                    bool see = pos < key1 && !(f.bad & (grp >= 2 ? 2 : 1));
-                    const int u = pos - base;
+                    const int pos = key + 16 * (e >> 2) + 4 * grp + (e & 3), u = pos - base;
+                    bool see = pos < key1 && !(bad >> (e >> 2) & 1);
                     if (!g.a.mask) {
                         see = see && u <= tok[mt];
                     } else if (see && u >= 0) {
                         see = tok[mt] < p.rows &&
                               g.a.mask[p.entry * g.a.mask_stride + tok[mt] * g.a.mask_ld + u] != 0;
                     }
-                    bits |= (uint32_t)see << e;
-                    if (!see) s[e >> 2][e & 3] = -INFINITY;
+                    vis[mt] |= (uint32_t)see << e;
+                    s[mt][e >> 2][e & 3] = see ? s[mt][e >> 2][e & 3] : -INFINITY;
                 }
-                vis[mt] = bits;
             }
-            float top = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])),
-                              fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3]))) *
-                        cs;
-            if (__any(top > ref[mt] + kSlack)) {
-                top = fmaxf(top, __shfl_xor(top, 16));
-                top = fmaxf(top, __shfl_xor(top, 32));
-                const float now = fmaxf(ref[mt], top);
-                const float keep = now == -INFINITY ? 1.f : exp2f(ref[mt] - now);
+        }
+        // Weights 2^(cs s + neg).  One beyond the slack, or any of a row whose
+        // reference is not set (neg infinite: its weights are infinite or NaN),
+        // gives its row a new reference; weights are positive, so their bits
+        // compare as integers.
+        float w[MT][8];
+        uint32_t most[MT] = {}, all = 0;
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                w[mt][i] = __builtin_amdgcn_exp2f(fmaf(s[mt][i >> 2][i & 3], cs, neg[mt]));
+                const uint32_t bits = __builtin_bit_cast(uint32_t, w[mt][i]);
+                most[mt] = bits > most[mt] ? bits : most[mt];
+            }
+            all = most[mt] > all ? most[mt] : all;
+        }
+        if (__any(all > kMostBits)) {
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) {
+                float now = s[mt][0][0];
+#pragma unroll
+                for (int i = 1; i < 8; ++i) now = fmaxf(now, s[mt][i >> 2][i & 3]);
+                now *= cs;
+                now = fmaxf(now, __shfl_xor(now, 16));
+                now = fmaxf(fmaxf(now, __shfl_xor(now, 32)), ref[mt]);
+                now = row_over(most[mt], kMostBits) ? now : ref[mt];
+                const float keep = now == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ref[mt] - now);
+                const float use = now == -INFINITY ? kLift : kLift - now;
                 ref[mt] = now;
-                neg[mt] = now == -INFINITY ? kLift : kLift - now;
+                neg[mt] = now == -INFINITY ? INFINITY : use;
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    w[mt][i] = __builtin_amdgcn_exp2f(fmaf(s[mt][i >> 2][i & 3], cs, use));
 #pragma unroll
                 for (int t = 0; t < DV; ++t) o[t][mt] *= keep;
                 lsum[mt] *= keep;
             }
-            float e[8];
+        }
+        u32x4 pf[MT];
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                e[i] = __builtin_amdgcn_exp2f(fmaf(s[i >> 2][i & 3], cs, neg[mt]));
+        for (int mt = 0; mt < MT; ++mt) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) pf[mt][i] = pack<F16>(e[2 * i], e[2 * i + 1]);
+            for (int i = 0; i < 4; ++i) pf[mt][i] = pack<F16>(w[mt][2 * i], w[mt][2 * i + 1]);
             lsum[mt] = mfma<F16>(ones, pf[mt], lsum[mt]);
         }
         // V^T: dims DV m + t of the lane's 8 keys.
         float unit[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) unit[i] = unit_of((f.vs[i >> 2] >> (8 * (i & 3))) & 0xFFu);
-        if (!plain) {
+        if constexpr (kMasked) {
             // A key that a row does not see leaves it alone even where its
             // value is NaN: such values count as 0 in the product, and the
-            // rows that do see them become NaN by a product of indicators.
+            // rows that do see them become NaN at the end, where a product of
+            // indicators has counted any.
             u32x4 nan = {0, 0, 0, 0};
             bool some = false;
 #pragma unroll
@@ -415,12 +461,7 @@ __global__ __launch_bounds__(kThreads) void kv_attention_kernel(Args g) {
                     for (int i = 0; i < 4; ++i)
                         seen[i] = ((vis[mt] >> (2 * i)) & 1 ? one & 0xFFFFu : 0u) |
                                   ((vis[mt] >> (2 * i + 1)) & 1 ? one & 0xFFFF0000u : 0u);
-                    const f32x4 hit = mfma<F16>(nan, seen, f32x4{0, 0, 0, 0});
-#pragma unroll
-                    for (int r = 0; r < 4; ++r)
-#pragma unroll
-                        for (int t = 0; t < DV; ++t)
-                            if (hit[r] > 0.f) o[t][mt][r] = NAN;
+                    hit[mt] = mfma<F16>(nan, seen, hit[mt]);
                 }
             }
         }
@@ -431,7 +472,7 @@ __global__ __launch_bounds__(kThreads) void kv_attention_kernel(Args g) {
                 uint32_t x[8];
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    const uint32_t word = f.v[D == 256 ? 2 * i + w : i];
+                    const uint32_t word = f.v[i >> 2][i & 3][w];
                     x[i] = by == 0   ? widen<F16, 0>(word, unit[i])
                            : by == 1 ? widen<F16, 1>(word, unit[i])
                            : by == 2 ? widen<F16, 2>(word, unit[i])
@@ -453,18 +494,30 @@ __global__ __launch_bounds__(kThreads) void kv_attention_kernel(Args g) {
         }
     };
 
+    // Steps that every row sees whole, the next step's bytes and the pages of
+    // the one behind it on their way while one is worked on; then the others.
     int key = key0 + wave * kStep;
-    if (key < key1) {
-        Step<D> cur, nxt;
-        load(cur, key);
-        for (;;) {
-            const int ahead = key + kTile;
-            if (ahead < key1) load(nxt, ahead);
-            compute(cur, key);
-            if (ahead >= key1) break;
-            cur = nxt;
-            key = ahead;
+    const int whole = (full < key1 ? full : key1) - kStep;     // last key of such a step
+    if (key <= whole) {
+        Step<D> f[2];
+        Pages now = pages(key), next = pages(key + kTile <= whole ? key + kTile : key);
+        load(f[0], now, key);
+        while (key <= whole && now.bad == 0) {
+            const int ahead = key + kTile <= whole ? key + kTile : key;
+            load(f[1], next, ahead);
+            const Pages then = pages(ahead + kTile <= whole ? ahead + kTile : ahead);
+            compute(f[0], 0, key, std::false_type{});
+            f[0] = f[1];
+            now = next;
+            next = then;
+            key += kTile;
         }
+    }
+    for (; key < key1; key += kTile) {
+        Step<D> f;
+        Pages now = pages(key);
+        load(f, now, key);
+        compute(f, now.bad, key, std::true_type{});
     }
 
     // The waves' sums to a common reference.
@@ -480,7 +533,8 @@ __global__ __launch_bounds__(kThreads) void kv_attention_kernel(Args g) {
 #pragma unroll
             for (int t = 0; t < DV; t += 4)
                 *(f32x4*)&s_o[wave][r][4 * DV * grp + DV * q + t] =
-                    f32x4{o[t][mt][q], o[t + 1][mt][q], o[t + 2][mt][q], o[t + 3][mt][q]};
+                    f32x4{o[t][mt][q], o[t + 1][mt][q], o[t + 2][mt][q], o[t + 3][mt][q]} +
+                    (hit[mt][q] > 0.f ? NAN : 0.f);
     }
     __syncthreads();
     for (int at = threadIdx.x; at < kRows * (D / 4); at += kThreads) {
@@ -514,29 +568,387 @@ __global__ __launch_bounds__(kThreads) void kv_attention_kernel(Args g) {
     }
 }
 
-// Joins the runs of a unit: RB rows of a tile for a workgroup, each row's runs
-// dealt to 4 / RB' waves.
-template <int D, bool F16, int MT, int RB>
+// The same for many rows (draft trees, prompt chunks): a workgroup's four
+// waves have 16 MT rows each and share the keys.  A tile of KT keys is widened
+// once for all of them and laid into LDS in the order in which the matrix
+// instructions take it (fragments of 16 bytes a lane: no conflicts), two tiles
+// in turn, so that one is read while the next is written; a wave widens 16
+// keys (or their keys or values alone).  Each wave ends with whole rows, so
+// nothing is joined but runs.
+template <int D, bool F16, int MT>
+__global__ __launch_bounds__(kThreads, 2) void kv_many_kernel(Args g) {
+    constexpr int kRows = 64 * MT;
+    constexpr int kKs = D / 32;
+    constexpr int DV = D / 16;
+    constexpr int KT = D * MT >= 256 ? 32 : 64;     // keys of a tile
+    constexpr int kTiles = KT / 16;
+    constexpr int kSteps = KT / 32;
+    __shared__ u32x4 s_k[2][kTiles][kKs][64];
+    __shared__ u32x4 s_v[2][kSteps][DV][64];
+    __shared__ u32x4 s_nan[2][kSteps][64];  // 1 where a value is NaN
+    __shared__ int s_flag[2][kTiles];       // 1: no page, 2: some value is NaN
+
+    const Plan p = plan<kRows>(g, -1);
+    if (p.entry < 0) return;
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int col = lane & 15, grp = lane >> 4;
+    const int n_tiles = (p.rows * g.group + kRows - 1) / kRows;
+    const int local = p.item - p.first;
+    const int rt = n_tiles - 1 - local % n_tiles;       // tiles that see the most keys first
+    const int head = (local / n_tiles) % g.c.heads;
+    const int split = local / n_tiles / g.c.heads;
+    const int r0 = rt * kRows;
+    const int w0 = r0 + wave * 16 * MT;         // the wave's rows
+    const int base = p.len - p.rows;
+    const int64_t start = kv_start(g.b, p.entry);
+
+    int tok[MT];
+    u32x4 qf[MT][kKs];
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+        const int r = w0 + mt * 16 + col;
+        tok[mt] = r / g.group;
+        const int64_t row = start + tok[mt];
+        const bool on = tok[mt] < p.rows && row >= 0 && row < g.b.n_rows;
+        const u32x4* src = (const u32x4*)((const uint16_t*)g.a.q + (on ? row : 0) * g.a.q_stride +
+                                          ((int64_t)head * g.group + r % g.group) * D +
+                                          grp * (D / 4));
+#pragma unroll
+        for (int s = 0; s < kKs; ++s) qf[mt][s] = on ? src[s] : u32x4{0, 0, 0, 0};
+    }
+
+    // Keys of the item; of a causal tile up to what its last row sees.  The
+    // wave's own rows see every key in front of `full` and none from `end` on.
+    const int key0 = split * p.run * kTile;
+    int key1 = p.splits == 1 ? p.len : key0 + p.run * kTile;
+    if (key1 > p.len) key1 = p.len;
+    int full = base, end = key1;
+    if (!g.a.mask) {
+        const int last = (r0 + kRows - 1) / g.group, mine = (w0 + 16 * MT - 1) / g.group;
+        const int seen = base + (last < p.rows ? last : p.rows - 1) + 1;
+        if (key1 > seen) key1 = seen;
+        const int own = base + (mine < p.rows ? mine : p.rows - 1) + 1;
+        full = base + w0 / g.group + 1;
+        end = own < key1 ? own : key1;
+    }
+    if (w0 / g.group >= p.rows) end = 0;        // no rows: the wave only widens
+
+    f32x4 o[DV][MT];
+    f32x4 lsum[MT];
+    f32x4 hit[MT];
+    float ref[MT], neg[MT];
+    constexpr float kLift = F16 ? 7.f : 0.f;
+    constexpr uint32_t kMostBits = (uint32_t)(127 + (F16 ? 15 : 8)) << 23;
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+#pragma unroll
+        for (int t = 0; t < DV; ++t) o[t][mt] = f32x4{0, 0, 0, 0};
+        lsum[mt] = f32x4{0, 0, 0, 0};
+        hit[mt] = f32x4{0, 0, 0, 0};
+        ref[mt] = -INFINITY;
+        neg[mt] = INFINITY;
+    }
+    const float cs = g.a.scale * 1.4426950408889634f;
+    const uint32_t one = F16 ? 0x3C003C00u : 0x3F803F80u;
+    const u32x4 ones = {one, one, one, one};
+
+    const ScalarInts table =
+        (ScalarInts)(uintptr_t)(g.c.page_table + (int64_t)p.seq * g.c.max_pages);
+    const int lg = g.c.lg_page, slot_mask = g.c.page() - 1;
+    const int64_t page_rows = (int64_t)2 * g.c.heads << lg;
+    const int64_t k_rows = g.c.rows_before(g.a.layer, 0, 0, head);
+    const int64_t v_rows = k_rows + ((int64_t)g.c.heads << lg);
+
+    // The wave's part of a tile: 16 keys, both products' side of them or one.
+    const int part = KT == 64 ? wave : wave >> 1;
+    const bool do_k = KT == 64 || (wave & 1) == 0, do_v = KT == 64 || (wave & 1) == 1;
+    uint32_t rk[D / 32], rks[D == 256 ? 2 : 1], rv[4][D == 256 ? 2 : 1], rvs;
+    int bad = 0;
+    auto fetch = [&](int key) {
+        int id = key + 16 * part < p.len ? table[(key + 16 * part) >> lg] : -1;
+        bad = !kv_page_ok(g.c, id);
+        if (bad) id = 0;
+        const int slot = (key + 16 * part) & slot_mask;
+        if (do_k) {
+            const int64_t kr = id * page_rows + k_rows;
+            const uint8_t* kc = g.c.codes + (kr + slot) * (D / 2) + col * (D / 2) + grp * (D / 8);
+            const uint8_t* ks = g.c.scales + kr * (D / 32) + slot + col +
+                                ((D == 64 ? grp >> 1 : (D == 128 ? grp : 2 * grp)) << lg);
+#pragma unroll
+            for (int w = 0; w < D / 32; ++w) rk[w] = ((const uint32_t*)kc)[w];
+#pragma unroll
+            for (int w = 0; w < (D == 256 ? 2 : 1); ++w) rks[w] = ks[w << lg];
+        }
+        if (do_v) {
+            const int64_t vr = id * page_rows + v_rows;
+            const uint8_t* vc =
+                g.c.codes + (vr + slot) * (D / 2) + 4 * grp * (D / 2) + col * (D / 32);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if constexpr (D == 64) {
+                    rv[i][0] = *(const uint16_t*)(vc + i * (D / 2));
+                } else {
+#pragma unroll
+                    for (int w = 0; w < D / 128; ++w)
+                        rv[i][w] = ((const uint32_t*)(vc + i * (D / 2)))[w];
+                }
+            }
+            rvs = *(const uint32_t*)(g.c.scales + vr * (D / 32) + slot + 4 * grp +
+                                     ((col * DV / 32) << lg));
+        }
+    };
+    auto spread = [&](int buf) {
+        if (do_k) {
+#pragma unroll
+            for (int q = 0; q < kKs; ++q)
+                s_k[buf][part][q][lane] = widen8<F16>(rk[q], unit_of(rks[D == 256 ? q >> 2 : 0]));
+        }
+        if (do_v) {
+            float unit[4];
+            bool some = false;
+            uint32_t nan[2] = {0, 0};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t byte = (rvs >> (8 * i)) & 0xFFu;
+                const bool here = byte == 255u;
+                some |= here;
+                nan[i >> 1] |= here ? (i & 1 ? one & 0xFFFF0000u : one & 0xFFFFu) : 0u;
+                unit[i] = here ? 0.f : unit_of(byte);
+            }
+            const int step = part >> 1, half = part & 1;
+            const bool any = __any(some);
+            if (lane == 0) s_flag[buf][part] = bad | (any ? 2 : 0);
+            ((u32x2*)&s_nan[buf][step][lane])[half] = u32x2{nan[0], nan[1]};
+#pragma unroll
+            for (int w = 0; w < (D == 256 ? 2 : 1); ++w)
+#pragma unroll
+                for (int by = 0; by < (D == 64 ? 2 : 4); ++by) {
+                    uint32_t x[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        x[i] = by == 0   ? widen<F16, 0>(rv[i][w], unit[i])
+                               : by == 1 ? widen<F16, 1>(rv[i][w], unit[i])
+                               : by == 2 ? widen<F16, 2>(rv[i][w], unit[i])
+                                         : widen<F16, 3>(rv[i][w], unit[i]);
+                    const int t = 8 * w + 2 * by;
+                    ((u32x2*)&s_v[buf][step][t][lane])[half] =
+                        u32x2{__builtin_amdgcn_perm(x[1], x[0], 0x05040100u),
+                              __builtin_amdgcn_perm(x[3], x[2], 0x05040100u)};
+                    ((u32x2*)&s_v[buf][step][t + 1][lane])[half] =
+                        u32x2{__builtin_amdgcn_perm(x[1], x[0], 0x07060302u),
+                              __builtin_amdgcn_perm(x[3], x[2], 0x07060302u)};
+                }
+        }
+    };
+
+    // One tile.  plain: every row of the wave sees all of it, and its flags are 0.
+    auto compute = [&](int buf, int key, int flags, bool plain) {
+        uint32_t vis[MT] = {};          // bit 4t + r: the row sees key 4 grp + r of quarter t
+        if (!plain) {
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt)
+                for (int e = 0; e < 4 * kTiles; ++e) {
+                    const int pos = key + 16 * (e >> 2) + 4 * grp + (e & 3), u = pos - base;
+                    bool see = pos < key1 && !(flags >> (2 * (e >> 2)) & 1);
+                    if (!g.a.mask) {
+                        see = see && u <= tok[mt];
+                    } else if (see && u >= 0) {
+                        see = tok[mt] < p.rows &&
+                              g.a.mask[p.entry * g.a.mask_stride + tok[mt] * g.a.mask_ld + u] != 0;
+                    }
+                    vis[mt] |= (uint32_t)see << e;
+                }
+        }
+        f32x4 s[MT][kTiles];
+        auto scores = [&]() {
+            // All reads on their way before the first product waits.
+            u32x4 kf[kKs][kTiles];
+#pragma unroll
+            for (int q = 0; q < kKs; ++q)
+#pragma unroll
+                for (int t = 0; t < kTiles; ++t) kf[q][t] = s_k[buf][t][q][lane];
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int q = 0; q < kKs; ++q)
+#pragma unroll
+                for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+                    for (int mt = 0; mt < MT; ++mt)
+                        s[mt][t] = mfma<F16>(kf[q][t], qf[mt][q], q ? s[mt][t] : f32x4{0, 0, 0, 0});
+            if (!plain) {
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                    for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r)
+                            s[mt][t][r] = vis[mt] >> (4 * t + r) & 1 ? s[mt][t][r] : -INFINITY;
+            }
+        };
+        scores();
+        uint32_t most[MT] = {}, all = 0;
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+#pragma unroll
+            for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    s[mt][t][r] = __builtin_amdgcn_exp2f(fmaf(s[mt][t][r], cs, neg[mt]));
+                    const float w = s[mt][t][r];
+                    const uint32_t bits = __builtin_bit_cast(uint32_t, w);
+                    most[mt] = bits > most[mt] ? bits : most[mt];
+                }
+            all = most[mt] > all ? most[mt] : all;
+        }
+        if (__any(all > kMostBits)) {
+            scores();                           // again: they are not kept
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) {
+                float now = s[mt][0][0];
+#pragma unroll
+                for (int i = 1; i < 4 * kTiles; ++i) now = fmaxf(now, s[mt][i >> 2][i & 3]);
+                now *= cs;
+                now = fmaxf(now, __shfl_xor(now, 16));
+                now = fmaxf(fmaxf(now, __shfl_xor(now, 32)), ref[mt]);
+                now = row_over(most[mt], kMostBits) ? now : ref[mt];
+                const float keep = now == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ref[mt] - now);
+                const float use = now == -INFINITY ? kLift : kLift - now;
+                ref[mt] = now;
+                neg[mt] = now == -INFINITY ? INFINITY : use;
+#pragma unroll
+                for (int i = 0; i < 4 * kTiles; ++i)
+                    s[mt][i >> 2][i & 3] =
+                        __builtin_amdgcn_exp2f(fmaf(s[mt][i >> 2][i & 3], cs, use));
+#pragma unroll
+                for (int t = 0; t < DV; ++t) o[t][mt] *= keep;
+                lsum[mt] *= keep;
+            }
+        }
+#pragma unroll
+        for (int step = 0; step < kSteps; ++step) {
+            constexpr int kBatch = DV < 8 ? DV : 8;
+            u32x4 pf[MT];
+#pragma unroll
+            for (int t0 = 0; t0 < DV; t0 += kBatch) {
+                u32x4 vf[kBatch];
+#pragma unroll
+                for (int t = 0; t < kBatch; ++t) vf[t] = s_v[buf][step][t0 + t][lane];
+                __builtin_amdgcn_sched_barrier(0);
+                if (t0 == 0) {
+#pragma unroll
+                    for (int mt = 0; mt < MT; ++mt) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            pf[mt][i] = pack<F16>(s[mt][2 * step + (i >> 1)][2 * i & 3],
+                                                  s[mt][2 * step + (i >> 1)][(2 * i & 3) + 1]);
+                        lsum[mt] = mfma<F16>(ones, pf[mt], lsum[mt]);
+                    }
+                }
+#pragma unroll
+                for (int t = 0; t < kBatch; ++t)
+#pragma unroll
+                    for (int mt = 0; mt < MT; ++mt)
+                        o[t0 + t][mt] = mfma<F16>(vf[t], pf[mt], o[t0 + t][mt]);
+            }
+            if (flags & (0xA << (4 * step))) {
+                const u32x4 nan = s_nan[buf][step][lane];
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt) {
+                    const uint32_t v = vis[mt] >> (8 * step);
+                    u32x4 seen;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        seen[i] = (v >> (2 * i) & 1 ? one & 0xFFFFu : 0u) |
+                                  (v >> (2 * i + 1) & 1 ? one & 0xFFFF0000u : 0u);
+                    hit[mt] = mfma<F16>(nan, seen, hit[mt]);
+                }
+            }
+        }
+    };
+
+    if (key0 < key1) {
+        fetch(key0);
+        spread(0);
+        if (key0 + KT < key1) fetch(key0 + KT);
+        __syncthreads();
+        int buf = 0;
+        for (int key = key0; key < key1; key += KT) {
+            // Flags of the tile's quarters, two bits each.
+            int flags = 0;
+#pragma unroll
+            for (int t = 0; t < kTiles; ++t) flags |= s_flag[buf][t] << (2 * t);
+            flags = __builtin_amdgcn_readfirstlane(flags);
+            if (key < end)
+                compute(buf, key, flags, key + KT <= full && key + KT <= end && flags == 0);
+            if (key + KT < key1) {
+                spread(buf ^ 1);
+                if (key + 2 * KT < key1) fetch(key + 2 * KT);
+                __syncthreads();
+            }
+            buf ^= 1;
+        }
+    }
+
+    // A lane has 4 DV neighbouring dims of each of its rows.
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+        const int r = wave * 16 * MT + mt * 16 + col, rr = r0 + r;
+        const int64_t row = start + tok[mt];
+        if (tok[mt] >= p.rows || row < 0 || row >= g.b.n_rows) continue;
+        const float l = lsum[mt][0];
+        if (p.splits == 1) {
+            const float inv = l == 0.f ? 0.f : 1.f / l;
+            u32x4* dst = (u32x4*)((uint16_t*)g.a.out + row * g.a.out_stride +
+                                  ((int64_t)head * g.group + rr % g.group) * D + 4 * DV * grp);
+#pragma unroll
+            for (int at = 0; at < 4 * DV; at += 8) {
+                u32x4 x;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int a = at + 2 * i, q = a / DV;
+                    const float nan = hit[mt][q] > 0.f ? NAN : 0.f;
+                    x[i] = pack<F16>(o[a % DV][mt][q] * inv + nan, o[a % DV + 1][mt][q] * inv + nan);
+                }
+                dst[at / 8] = x;
+            }
+        } else {
+            float* dst = g.part_o + ((int64_t)p.item * kRows + r) * D + 4 * DV * grp;
+#pragma unroll
+            for (int at = 0; at < 4 * DV; at += 4) {
+                const int q = at / DV, t = at % DV;
+                *(f32x4*)(dst + at) =
+                    f32x4{o[t][mt][q], o[t + 1][mt][q], o[t + 2][mt][q], o[t + 3][mt][q]} +
+                    (hit[mt][q] > 0.f ? NAN : 0.f);
+            }
+            if (grp == 0) g.part_ml[(int64_t)p.item * kRows + r] = f32x2{ref[mt], l};
+        }
+    }
+}
+
+// Joins the runs of a unit: RB rows of a tile of ROWS for a workgroup.  RB 1:
+// the row's runs are dealt to teams of threads, who add up at the end; else
+// each row has a team.
+template <int D, bool F16, int ROWS, int RB>
 __global__ __launch_bounds__(kThreads) void kv_join_kernel(Args g, int tiles_max) {
-    constexpr int kRows = 16 * MT;
     constexpr int kLanes = D / 4;                 // threads of a row
     constexpr int kTeams = kThreads / kLanes;     // 16, 8, 4
     __shared__ f32x4 s_o[kTeams][kLanes];
     __shared__ f32x2 s_ml[kTeams];
-    const int per_tile = kRows / RB;
-    const int sub = blockIdx.x % per_tile;
-    const int rt = blockIdx.x / per_tile % tiles_max;
-    const int head = blockIdx.x / per_tile / tiles_max % g.c.heads;
-    const int entry = blockIdx.x / per_tile / tiles_max / g.c.heads;
-    const Plan p = plan<kRows>(g, entry);
+    constexpr int kPer = RB == 1 ? 16 : ROWS / RB;    // workgroups of a tile
+    const int sub = blockIdx.x % kPer;
+    const int rt = blockIdx.x / kPer % tiles_max;
+    const int head = blockIdx.x / kPer / tiles_max % g.c.heads;
+    const int entry = blockIdx.x / kPer / tiles_max / g.c.heads;
+    const Plan p = plan<ROWS>(g, entry);
     if (p.entry < 0 || p.splits == 1) return;
-    const int n_tiles = (p.rows * g.group + kRows - 1) / kRows;
+    const int n_tiles = (p.rows * g.group + ROWS - 1) / ROWS;
     if (rt >= n_tiles) return;
+    const int place = ROWS <= 32 ? rt : n_tiles - 1 - rt;
     const int team = threadIdx.x / kLanes, dim = threadIdx.x % kLanes * 4;
     const int64_t start = kv_start(g.b, p.entry);
-    // RB == 1: the teams share a row's runs.  Else a team has rows of its own.
     for (int r = sub * RB + (RB == 1 ? 0 : team); r < (sub + 1) * RB; r += kTeams) {
-        const int rr = rt * kRows + r, token = rr / g.group;
+        const int rr = rt * ROWS + r, token = rr / g.group;
         const int64_t row = start + token;
         const bool on = token < p.rows && row >= 0 && row < g.b.n_rows;
         if (RB == 1 && !on) return;               // the whole workgroup
@@ -547,7 +959,7 @@ __global__ __launch_bounds__(kThreads) void kv_join_kernel(Args g, int tiles_max
 #pragma unroll 4
             for (int s = RB == 1 ? team : 0; s < p.splits; s += step) {
                 const int64_t at =
-                    ((int64_t)p.first + (s * g.c.heads + head) * n_tiles + rt) * kRows + r;
+                    ((int64_t)p.first + (s * g.c.heads + head) * n_tiles + place) * ROWS + r;
                 const f32x2 ml = g.part_ml[at];
                 const f32x4 x = *(const f32x4*)(g.part_o + at * D + dim);
                 const float now = fmaxf(top, ml[0]);
@@ -582,50 +994,51 @@ __global__ __launch_bounds__(kThreads) void kv_join_kernel(Args g, int tiles_max
     }
 }
 
-// Row tiles of a wave: as many as the rows of a unit fill, up to 64 rows (32
-// of 256 dims, whose sums take twice the registers).  A tile of more rows
-// widens each key and value once for all of them.
-int row_tiles(int max_rows, int group, int d) {
+// Rows of a tile.  Up to 32 rows of a unit are one tile of the kernel whose
+// waves share rows; more go to the one whose waves share keys, in tiles of 128
+// (of 64 where the unit has no more, and of 256 dims, whose sums take twice
+// the registers).
+int tile_rows(int max_rows, int group, int d) {
     const int64_t rows = (int64_t)max_rows * group;
-    const int most = d == 256 ? 2 : 4;
-    const int mt = rows <= 16 ? 1 : (rows <= 32 ? 2 : 4);
-    return mt < most ? mt : most;
+    if (rows <= 16) return 16;
+    if (rows <= 32 && d != 256) return 32;
+    return rows <= 64 || d == 256 ? 64 : 128;
 }
 
 // Workgroups to cut the work for: what is resident at once.
-int target_items(int mt) { return device_cus() * (mt == 1 ? 4 : (mt == 2 ? 2 : 1)); }
+int target_items(int rows) { return device_cus() * (rows == 16 ? 4 : 2); }
 
-int64_t units_most(int n, int max_rows, int n_heads, int kv_heads, int mt) {
-    const int64_t tiles = ((int64_t)max_rows * (n_heads / kv_heads) + 16 * mt - 1) / (16 * mt);
+int64_t units_most(int n, int max_rows, int n_heads, int kv_heads, int rows) {
+    const int64_t tiles = ((int64_t)max_rows * (n_heads / kv_heads) + rows - 1) / rows;
     return tiles * kv_heads * n;
 }
 
-template <int D, bool F16, int MT>
-hipError_t launch_mt(const Args& g, hipStream_t st) {
-    const int64_t units = units_most(g.b.n, g.b.max_rows, g.a.n_heads, g.c.heads, MT);
-    // ceil(total / 8) workgroups for each XCD; total <= target + units.
-    const int64_t most = units + g.target;
-    hipLaunchKernelGGL((kv_attention_kernel<D, F16, MT>), dim3((unsigned)((most + 7) / 8 * 8)),
-                       dim3(kThreads), 0, st, g);
+template <int D, bool F16, int ROWS>
+hipError_t launch_rows(const Args& g, hipStream_t st) {
+    const int64_t units = units_most(g.b.n, g.b.max_rows, g.a.n_heads, g.c.heads, ROWS);
+    // Whole runs for every XCD; at most target + units items.
+    const int64_t per = ROWS <= 32 ? 8 : 8 * kXcdRun;
+    const dim3 grid((unsigned)((units + g.target + per - 1) / per * per));
+    if constexpr (ROWS <= 32)
+        hipLaunchKernelGGL((kv_few_kernel<D, F16, ROWS / 16>), grid, dim3(kThreads), 0, st, g);
+    else
+        hipLaunchKernelGGL((kv_many_kernel<D, F16, ROWS / 64>), grid, dim3(kThreads), 0, st, g);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || !g.target) return e;
     const int tiles = (int)(units / g.c.heads / g.b.n);
-    const int64_t rows = (int64_t)g.b.max_rows * g.group;
-    if (rows <= 16) {
-        hipLaunchKernelGGL((kv_join_kernel<D, F16, MT, 1>), dim3((unsigned)(units * 16 * MT)),
-                           dim3(kThreads), 0, st, g, tiles);
-    } else {
-        hipLaunchKernelGGL((kv_join_kernel<D, F16, MT, 16>), dim3((unsigned)(units * MT)),
-                           dim3(kThreads), 0, st, g, tiles);
-    }
+    constexpr int RB = ROWS == 16 ? 1 : 16;
+    constexpr int kPer = RB == 1 ? 16 : ROWS / RB;
+    hipLaunchKernelGGL((kv_join_kernel<D, F16, ROWS, RB>), dim3((unsigned)(units * kPer)),
+                       dim3(kThreads), 0, st, g, tiles);
     return hipGetLastError();
 }
 
 template <int D, bool F16>
-hipError_t launch_d(Args& g, int mt, hipStream_t st) {
-    if (mt == 1) return launch_mt<D, F16, 1>(g, st);
-    if (mt == 2) return launch_mt<D, F16, 2>(g, st);
-    if constexpr (D != 256) return launch_mt<D, F16, 4>(g, st);
+hipError_t launch_d(const Args& g, int rows, hipStream_t st) {
+    if (rows == 16) return launch_rows<D, F16, 16>(g, st);
+    if (rows == 64) return launch_rows<D, F16, 64>(g, st);
+    if constexpr (D != 256)
+        return rows == 32 ? launch_rows<D, F16, 32>(g, st) : launch_rows<D, F16, 128>(g, st);
     return hipErrorInvalidValue;
 }
 
@@ -634,20 +1047,19 @@ size_t align256(size_t x) { return (x + 255) / 256 * 256; }
 }  // namespace
 
 int64_t kv_attention_blocks(int n, int max_rows, int n_heads, int kv_heads, int d) {
-    const int mt = row_tiles(max_rows, n_heads / kv_heads, d);
-    const int64_t units = units_most(n, max_rows, n_heads, kv_heads, mt);
+    const int rows = tile_rows(max_rows, n_heads / kv_heads, d);
+    const int64_t units = units_most(n, max_rows, n_heads, kv_heads, rows);
     // Of the attention itself, and of the join (a workgroup for 1 or 16 rows).
-    return units * ((int64_t)max_rows * (n_heads / kv_heads) <= 16 ? 16 * mt : mt) +
-           target_items(mt);
+    return units * (rows == 16 ? 16 : rows / 16) + target_items(rows) + 8 * kXcdRun;
 }
 
 size_t kv_attention_workspace_bytes(int n, int max_rows, int n_heads, int kv_heads, int d,
                                     int max_kv) {
     if (max_kv <= kMinRun) return 0;
-    const int mt = row_tiles(max_rows, n_heads / kv_heads, d);
-    const int64_t items = units_most(n, max_rows, n_heads, kv_heads, mt) + target_items(mt);
-    const size_t rows = (size_t)items * 16 * mt;
-    return align256(rows * d * sizeof(float)) + align256(rows * sizeof(f32x2));
+    const int rows = tile_rows(max_rows, n_heads / kv_heads, d);
+    const int64_t items = units_most(n, max_rows, n_heads, kv_heads, rows) + target_items(rows);
+    return align256((size_t)items * rows * d * sizeof(float)) +
+           align256((size_t)items * rows * sizeof(f32x2));
 }
 
 hipError_t launch_kv_attention(const KvCache& c, const KvBatch& b, const KvAttention& a,
@@ -657,16 +1069,17 @@ hipError_t launch_kv_attention(const KvCache& c, const KvBatch& b, const KvAtten
     g.b = b;
     g.a = a;
     g.group = a.n_heads / c.heads;
-    const int mt = row_tiles(b.max_rows, g.group, c.d);
-    g.target = a.max_kv > kMinRun ? target_items(mt) : 0;
-    const int64_t items = units_most(b.n, b.max_rows, a.n_heads, c.heads, mt) + g.target;
+    const int rows = tile_rows(b.max_rows, g.group, c.d);
+    g.target = a.max_kv > kMinRun ? target_items(rows) : 0;
+    const int64_t items = units_most(b.n, b.max_rows, a.n_heads, c.heads, rows) + g.target;
     g.part_o = (float*)workspace;
-    g.part_ml = (f32x2*)((char*)workspace +
-                         align256((size_t)items * 16 * mt * c.d * sizeof(float)));
+    g.part_ml =
+        (f32x2*)((char*)workspace + align256((size_t)items * rows * c.d * sizeof(float)));
     const bool f16 = a.dtype == DT_F16;
-    if (c.d == 64) return f16 ? launch_d<64, true>(g, mt, st) : launch_d<64, false>(g, mt, st);
-    if (c.d == 128) return f16 ? launch_d<128, true>(g, mt, st) : launch_d<128, false>(g, mt, st);
-    return f16 ? launch_d<256, true>(g, mt, st) : launch_d<256, false>(g, mt, st);
+    if (c.d == 64) return f16 ? launch_d<64, true>(g, rows, st) : launch_d<64, false>(g, rows, st);
+    if (c.d == 128)
+        return f16 ? launch_d<128, true>(g, rows, st) : launch_d<128, false>(g, rows, st);
+    return f16 ? launch_d<256, true>(g, rows, st) : launch_d<256, false>(g, rows, st);
 }
 
 }  // namespace sense
