@@ -33,8 +33,6 @@
 // in its range.  Probabilities are rounded to the query's type (nearest);
 // their sum is taken of the rounded ones, by a product with ones, so that the
 // weights that are used add up to 1.
-#include <type_traits>
-
 #include "internal.h"
 #include "kv.h"
 
@@ -48,11 +46,15 @@ constexpr int kTile = kStep * kWaves;  // keys of a workgroup's step
 // A unit is not cut below this many keys: a shorter run costs more in joining
 // than its parallelism gains.
 constexpr int kMinRun = 256;
+// Nor is any where no sequence is longer than this: a second launch takes
+// longer than the keys.
+constexpr int kWhole = 1024;
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
@@ -61,6 +63,7 @@ typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 // The page table is not written while these kernels run: scalar loads.
 typedef const __attribute__((address_space(4))) int32_t* ScalarInts;
 
+constexpr int kTries = 3;              // run lengths tried
 constexpr int kXcdRun = 8;             // items of a run (tiles of more than 32 rows)
 
 struct Args {
@@ -71,6 +74,7 @@ struct Args {
     int target;         // workgroups that the work is cut for (0: units stay whole)
     float* part_o;      // [item][rows][d]
     f32x2* part_ml;     // [item][rows]: reference, sum
+    i32x4* plans;       // [entry]: new tokens, first item, runs of a unit
 };
 
 // Where one unit tile's items lie, and which keys one of them has.
@@ -90,51 +94,74 @@ __device__ __forceinline__ int64_t wave_sum64(int64_t v) {
 }
 
 // The items of the entries, in order, computed by every wave for itself from
-// the entries' lengths.  entry < 0: the entry that this workgroup's item
-// belongs to; else that entry.  Workgroups are dealt to the 8 XCDs in turn;
-// items go to them in short runs, so that tiles which read the same keys share
-// an L2 and every XCD still has its part of each entry.
+// the entries' lengths, and the one of this workgroup.  Workgroups are dealt
+// to the 8 XCDs in turn; items go to them in short runs, so that tiles which
+// read the same keys share an L2 and every XCD still has its part of each
+// entry.  The first workgroup leaves the entries' items for the join.
 template <int ROWS>
-__device__ __forceinline__ Plan plan(const Args& g, int entry) {
+__device__ __forceinline__ Plan plan(const Args& g) {
     const int lane = threadIdx.x & 63;
     const int n = g.b.n, per = (n + 63) / 64;
     const int e0 = lane * per < n ? lane * per : n;
     const int e1 = e0 + per < n ? e0 + per : n;
-    int64_t work = 0;
+    int64_t work = 0, whole = 0;
     for (int e = e0; e < e1; ++e) {
         const int s = kv_seq(g.c, g.b.seqs, e);
         if (s < 0) continue;
         const int m = kv_rows(g.b, e);
         const int units = (m * g.group + ROWS - 1) / ROWS;
         work += (int64_t)units * ((kv_length(g.c, s) + kTile - 1) / kTile);
+        whole += units;
     }
     work = wave_sum64(work) * g.c.heads;
+    whole = wave_sum64(whole) * g.c.heads;
     int64_t run64 = g.target ? (work + g.target - 1) / g.target : 1 << 24;
     if (run64 < kMinRun / kTile) run64 = kMinRun / kTile;
     Plan p;
     p.run = __builtin_amdgcn_readfirstlane((int)(run64 < (1 << 24) ? run64 : (1 << 24)));
-    int mine = 0;
-    for (int e = e0; e < e1; ++e) {
-        const int s = kv_seq(g.c, g.b.seqs, e);
-        if (s < 0) continue;
-        const int units = (kv_rows(g.b, e) * g.group + ROWS - 1) / ROWS;
-        const int tiles = (kv_length(g.c, s) + kTile - 1) / kTile;
-        const int splits = tiles > p.run ? (tiles + p.run - 1) / p.run : 1;
-        mine += units * splits * g.c.heads;
-    }
-    int upto = mine;
+    // Items of the lane's entries with runs of that length.  Rounding up makes
+    // more of them than `target`, and the last few would have the device to
+    // themselves: the runs are made longer until they fit (or units are whole).
+    int mine, upto, total;
+    for (int tries = 0;; ++tries) {
+        mine = 0;
+        for (int e = e0; e < e1; ++e) {
+            const int s = kv_seq(g.c, g.b.seqs, e);
+            if (s < 0) continue;
+            const int units = (kv_rows(g.b, e) * g.group + ROWS - 1) / ROWS;
+            const int tiles = (kv_length(g.c, s) + kTile - 1) / kTile;
+            const int splits = tiles > p.run ? (tiles + p.run - 1) / p.run : 1;
+            mine += units * splits * g.c.heads;
+        }
+        upto = mine;
 #pragma unroll
-    for (int s = 1; s < 64; s <<= 1) {
-        const int o = __shfl_up(upto, s);
-        if (lane >= s) upto += o;
+        for (int s = 1; s < 64; s <<= 1) {
+            const int o = __shfl_up(upto, s);
+            if (lane >= s) upto += o;
+        }
+        total = __builtin_amdgcn_readlane(upto, 63);
+        if (total <= g.target || whole >= g.target || tries == kTries) break;
+        const int longer = (int)((int64_t)p.run * total / g.target);
+        p.run = __builtin_amdgcn_readfirstlane(longer > p.run ? longer : p.run + 1);
     }
+    p.run = __builtin_amdgcn_readfirstlane(p.run);
     constexpr int kRun = ROWS <= 32 ? 1 : kXcdRun;
     const int idx = (int)(blockIdx.x >> 3);
     const int item = ((idx / kRun) * 8 + (int)(blockIdx.x & 7)) * kRun + idx % kRun;
     p.item = item;
-    const bool owner = entry < 0 ? (item >= upto - mine && item < upto)
-                                 : (entry >= e0 && entry < e1);
-    const uint64_t who = __ballot(owner);
+    if (g.target && blockIdx.x == 0 && threadIdx.x < 64) {
+        int at = upto - mine;
+        for (int e = e0; e < e1; ++e) {
+            const int s = kv_seq(g.c, g.b.seqs, e);
+            const int m = s < 0 ? 0 : kv_rows(g.b, e);
+            const int units = (m * g.group + ROWS - 1) / ROWS;
+            const int tiles = s < 0 ? 0 : (kv_length(g.c, s) + kTile - 1) / kTile;
+            const int splits = tiles > p.run ? (tiles + p.run - 1) / p.run : 1;
+            g.plans[e] = i32x4{m, at, splits, 0};
+            at += units * splits * g.c.heads;
+        }
+    }
+    const uint64_t who = __ballot(item >= upto - mine && item < upto);
     p.entry = -1;
     p.seq = -1;
     p.rows = p.len = p.first = 0;
@@ -153,7 +180,7 @@ __device__ __forceinline__ Plan plan(const Args& g, int entry) {
         const int tiles = (len + kTile - 1) / kTile;
         const int splits = tiles > p.run ? (tiles + p.run - 1) / p.run : 1;
         const int mine_e = units * splits * g.c.heads;
-        if (entry < 0 ? item < at + mine_e : e == entry) {
+        if (item < at + mine_e) {
             p.entry = __builtin_amdgcn_readfirstlane(e);
             p.seq = __builtin_amdgcn_readfirstlane(s);
             p.rows = __builtin_amdgcn_readfirstlane(m);
@@ -216,6 +243,37 @@ __device__ __forceinline__ float unit_of(uint32_t byte) {
     return __builtin_bit_cast(float, byte << 23);
 }
 
+// Which of 4 N positions a row sees: bit 4t + r is position first + 16t + r,
+// with `none` the tiles that have no page (bit `stride` t).  The mask's bytes
+// are read together, from places inside it whether they count or not.
+template <int N>
+__device__ __forceinline__ uint32_t seen_bits(const Args& g, const Plan& p, int token, int first,
+                                              int end, uint32_t none, int stride) {
+    const int base = p.len - p.rows;
+    uint8_t byte[4 * N];
+    if (g.a.mask) {
+        const int row = token < p.rows ? token : p.rows - 1;
+        const uint8_t* m = g.a.mask + p.entry * g.a.mask_stride + row * g.a.mask_ld;
+#pragma unroll
+        for (int e = 0; e < 4 * N; ++e) {
+            const int u = first + 16 * (e >> 2) + (e & 3) - base;
+            byte[e] = m[u < 0 ? 0 : (u < p.rows ? u : p.rows - 1)];
+        }
+    }
+    uint32_t bits = 0;
+#pragma unroll
+    for (int e = 0; e < 4 * N; ++e) {
+        const int pos = first + 16 * (e >> 2) + (e & 3), u = pos - base;
+        bool see = pos < end && !(none >> (stride * (e >> 2)) & 1);
+        if (!g.a.mask)
+            see = see && u <= token;
+        else
+            see = see && (u < 0 || (byte[e] != 0 && token < p.rows));
+        bits |= (uint32_t)see << e;
+    }
+    return bits;
+}
+
 // One step's codes and scales of a lane.
 template <int D>
 struct Step {
@@ -232,7 +290,7 @@ struct Pages {
 };
 
 template <int D, bool F16, int MT>
-__global__ __launch_bounds__(kThreads, MT * D > 128 ? 2 : (MT == 2 ? 3 : 4)) void kv_few_kernel(Args g) {
+__global__ __launch_bounds__(kThreads, MT * D > 128 || MT == 2 ? 2 : (D == 128 ? 3 : 4)) void kv_few_kernel(Args g) {
     constexpr int kRows = 16 * MT;
     constexpr int kKs = D / 32;         // matrix steps of the first product
     constexpr int DV = D / 16;          // dims of a lane in the second
@@ -241,7 +299,7 @@ __global__ __launch_bounds__(kThreads, MT * D > 128 ? 2 : (MT == 2 ? 3 : 4)) voi
     __shared__ float s_m[kWaves][kRows];
     __shared__ float s_l[kWaves][kRows];
 
-    const Plan p = plan<kRows>(g, -1);
+    const Plan p = plan<kRows>(g);
     if (p.entry < 0) return;
     const int item = p.item;
 
@@ -354,9 +412,8 @@ __global__ __launch_bounds__(kThreads, MT * D > 128 ? 2 : (MT == 2 ? 3 : 4)) voi
         }
     };
 
-    // One step of 32 keys.  MASKED: some row does not see some key of it.
-    auto compute = [&](const Step<D>& f, int bad, int key, auto masked) {
-        constexpr bool kMasked = decltype(masked)::value;
+    // One step of 32 keys.  plain: every row sees every key of it.
+    auto compute = [&](const Step<D>& f, int bad, int key, bool plain) {
         // S^T: two tiles of 16 keys.
         f32x4 s[MT][2];
 #pragma unroll
@@ -372,22 +429,13 @@ __global__ __launch_bounds__(kThreads, MT * D > 128 ? 2 : (MT == 2 ? 3 : 4)) voi
                     s[mt][t] = mfma<F16>(kf[t], qf[mt][q], q ? s[mt][t] : f32x4{0, 0, 0, 0});
         }
         uint32_t vis[MT] = {};          // bit 4t + r: the row sees key 4 grp + r of tile t
-        if constexpr (kMasked) {
+        if (!plain) {
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) {
+                vis[mt] = seen_bits<2>(g, p, tok[mt], key + 4 * grp, key1, bad, 1);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const int pos = key + 16 * (e >> 2) + 4 * grp + (e & 3), u = pos - base;
-                    bool see = pos < key1 && !(bad >> (e >> 2) & 1);
-                    if (!g.a.mask) {
-                        see = see && u <= tok[mt];
-                    } else if (see && u >= 0) {
-                        see = tok[mt] < p.rows &&
-                              g.a.mask[p.entry * g.a.mask_stride + tok[mt] * g.a.mask_ld + u] != 0;
-                    }
-                    vis[mt] |= (uint32_t)see << e;
-                    s[mt][e >> 2][e & 3] = see ? s[mt][e >> 2][e & 3] : -INFINITY;
-                }
+                for (int e = 0; e < 8; ++e)
+                    s[mt][e >> 2][e & 3] = vis[mt] >> e & 1 ? s[mt][e >> 2][e & 3] : -INFINITY;
             }
         }
         // Weights 2^(cs s + neg).  One beyond the slack, or any of a row whose
@@ -439,7 +487,7 @@ __global__ __launch_bounds__(kThreads, MT * D > 128 ? 2 : (MT == 2 ? 3 : 4)) voi
         float unit[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) unit[i] = unit_of((f.vs[i >> 2] >> (8 * (i & 3))) & 0xFFu);
-        if constexpr (kMasked) {
+        if (!plain) {
             // A key that a row does not see leaves it alone even where its
             // value is NaN: such values count as 0 in the product, and the
             // rows that do see them become NaN at the end, where a product of
@@ -494,30 +542,23 @@ __global__ __launch_bounds__(kThreads, MT * D > 128 ? 2 : (MT == 2 ? 3 : 4)) voi
         }
     };
 
-    // Steps that every row sees whole, the next step's bytes and the pages of
-    // the one behind it on their way while one is worked on; then the others.
+    // The next step's bytes and the pages of the one behind it are on their way
+    // while a step is worked on.
     int key = key0 + wave * kStep;
-    const int whole = (full < key1 ? full : key1) - kStep;     // last key of such a step
-    if (key <= whole) {
+    if (key < key1) {
         Step<D> f[2];
-        Pages now = pages(key), next = pages(key + kTile <= whole ? key + kTile : key);
+        Pages now = pages(key), next = pages(key + kTile < key1 ? key + kTile : key);
         load(f[0], now, key);
-        while (key <= whole && now.bad == 0) {
-            const int ahead = key + kTile <= whole ? key + kTile : key;
+        while (key < key1) {
+            const int ahead = key + kTile < key1 ? key + kTile : key;
             load(f[1], next, ahead);
-            const Pages then = pages(ahead + kTile <= whole ? ahead + kTile : ahead);
-            compute(f[0], 0, key, std::false_type{});
+            const Pages then = pages(ahead + kTile < key1 ? ahead + kTile : ahead);
+            compute(f[0], now.bad, key, key + kStep <= full && key + kStep <= key1 && now.bad == 0);
             f[0] = f[1];
             now = next;
             next = then;
             key += kTile;
         }
-    }
-    for (; key < key1; key += kTile) {
-        Step<D> f;
-        Pages now = pages(key);
-        load(f, now, key);
-        compute(f, now.bad, key, std::true_type{});
     }
 
     // The waves' sums to a common reference.
@@ -550,7 +591,8 @@ __global__ __launch_bounds__(kThreads, MT * D > 128 ? 2 : (MT == 2 ? 3 : 4)) voi
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) {
             // A wave that saw no key has sums of 0 (or of NaN scores).
-            const float f = s_m[w][r] == -INFINITY ? 1.f : exp2f(s_m[w][r] - top);
+            const float f =
+                s_m[w][r] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(s_m[w][r] - top);
             l += s_l[w][r] * f;
             sum += *(const f32x4*)&s_o[w][r][dim] * f;
         }
@@ -588,7 +630,7 @@ __global__ __launch_bounds__(kThreads, 2) void kv_many_kernel(Args g) {
     __shared__ u32x4 s_nan[2][kSteps][64];  // 1 where a value is NaN
     __shared__ int s_flag[2][kTiles];       // 1: no page, 2: some value is NaN
 
-    const Plan p = plan<kRows>(g, -1);
+    const Plan p = plan<kRows>(g);
     if (p.entry < 0) return;
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -748,17 +790,7 @@ __global__ __launch_bounds__(kThreads, 2) void kv_many_kernel(Args g) {
         if (!plain) {
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt)
-                for (int e = 0; e < 4 * kTiles; ++e) {
-                    const int pos = key + 16 * (e >> 2) + 4 * grp + (e & 3), u = pos - base;
-                    bool see = pos < key1 && !(flags >> (2 * (e >> 2)) & 1);
-                    if (!g.a.mask) {
-                        see = see && u <= tok[mt];
-                    } else if (see && u >= 0) {
-                        see = tok[mt] < p.rows &&
-                              g.a.mask[p.entry * g.a.mask_stride + tok[mt] * g.a.mask_ld + u] != 0;
-                    }
-                    vis[mt] |= (uint32_t)see << e;
-                }
+                vis[mt] = seen_bits<kTiles>(g, p, tok[mt], key + 4 * grp, key1, flags, 2);
         }
         f32x4 s[MT][kTiles];
         auto scores = [&]() {
@@ -930,43 +962,59 @@ __global__ __launch_bounds__(kThreads, 2) void kv_many_kernel(Args g) {
 // the row's runs are dealt to teams of threads, who add up at the end; else
 // each row has a team.
 template <int D, bool F16, int ROWS, int RB>
-__global__ __launch_bounds__(kThreads) void kv_join_kernel(Args g, int tiles_max) {
+__global__ __launch_bounds__(kThreads) void kv_join_kernel(Args g, int tiles_max, int per_tile) {
     constexpr int kLanes = D / 4;                 // threads of a row
     constexpr int kTeams = kThreads / kLanes;     // 16, 8, 4
     __shared__ f32x4 s_o[kTeams][kLanes];
     __shared__ f32x2 s_ml[kTeams];
-    constexpr int kPer = RB == 1 ? 16 : ROWS / RB;    // workgroups of a tile
-    const int sub = blockIdx.x % kPer;
-    const int rt = blockIdx.x / kPer % tiles_max;
-    const int head = blockIdx.x / kPer / tiles_max % g.c.heads;
-    const int entry = blockIdx.x / kPer / tiles_max / g.c.heads;
-    const Plan p = plan<ROWS>(g, entry);
-    if (p.entry < 0 || p.splits == 1) return;
-    const int n_tiles = (p.rows * g.group + ROWS - 1) / ROWS;
+    const int sub = blockIdx.x % per_tile;
+    const int rt = blockIdx.x / per_tile % tiles_max;
+    const int head = blockIdx.x / per_tile / tiles_max % g.c.heads;
+    const int entry = blockIdx.x / per_tile / tiles_max / g.c.heads;
+    const i32x4 plan = g.plans[entry];
+    const int rows = plan[0], first_item = plan[1], splits = plan[2];
+    if (splits == 1) return;
+    const int n_tiles = (rows * g.group + ROWS - 1) / ROWS;
     if (rt >= n_tiles) return;
     const int place = ROWS <= 32 ? rt : n_tiles - 1 - rt;
     const int team = threadIdx.x / kLanes, dim = threadIdx.x % kLanes * 4;
-    const int64_t start = kv_start(g.b, p.entry);
+    const int64_t start = kv_start(g.b, entry);
     for (int r = sub * RB + (RB == 1 ? 0 : team); r < (sub + 1) * RB; r += kTeams) {
         const int rr = rt * ROWS + r, token = rr / g.group;
         const int64_t row = start + token;
-        const bool on = token < p.rows && row >= 0 && row < g.b.n_rows;
+        const bool on = token < rows && row >= 0 && row < g.b.n_rows;
         if (RB == 1 && !on) return;               // the whole workgroup
         float top = -INFINITY, l = 0.f;
         f32x4 sum = {0, 0, 0, 0};
         if (on) {
-            const int step = RB == 1 ? kTeams : 1;
-#pragma unroll 4
-            for (int s = RB == 1 ? team : 0; s < p.splits; s += step) {
-                const int64_t at =
-                    ((int64_t)p.first + (s * g.c.heads + head) * n_tiles + place) * ROWS + r;
-                const f32x2 ml = g.part_ml[at];
-                const f32x4 x = *(const f32x4*)(g.part_o + at * D + dim);
-                const float now = fmaxf(top, ml[0]);
-                const float a = top == -INFINITY ? 1.f : exp2f(top - now);
-                const float b = ml[0] == -INFINITY ? 1.f : exp2f(ml[0] - now);
-                l = l * a + ml[1] * b;
-                sum = sum * a + x * b;
+            // The partial sums come from far (other XCDs wrote them): many at
+            // a time; places behind the last read the first again, weight 0.
+            constexpr int kEvery = RB == 1 ? kTeams : 1, kBatch = RB == 1 ? 16 : 8;
+            const int64_t first = ((int64_t)first_item + head * n_tiles + place) * ROWS + r;
+            const int64_t apart = (int64_t)g.c.heads * n_tiles * ROWS;
+            for (int s0 = RB == 1 ? team : 0; s0 < splits; s0 += kBatch * kEvery) {
+                f32x2 ml[kBatch];
+                f32x4 x[kBatch];
+#pragma unroll
+                for (int i = 0; i < kBatch; ++i) {
+                    const int s = s0 + i * kEvery;
+                    const int64_t at = first + (s < splits ? s : s0) * apart;
+                    ml[i] = g.part_ml[at];
+                    x[i] = *(const f32x4*)(g.part_o + at * D + dim);
+                }
+                float now = top;
+#pragma unroll
+                for (int i = 0; i < kBatch; ++i) now = fmaxf(now, ml[i][0]);
+                const float a = top == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(top - now);
+                l *= a;
+                sum *= a;
+#pragma unroll
+                for (int i = 0; i < kBatch; ++i) {
+                    float w = ml[i][0] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ml[i][0] - now);
+                    w = s0 + i * kEvery < splits ? w : 0.f;
+                    l += ml[i][1] * w;
+                    sum += x[i] * w;
+                }
                 top = now;
             }
         }
@@ -977,8 +1025,9 @@ __global__ __launch_bounds__(kThreads) void kv_join_kernel(Args g, int tiles_max
             if (team != 0) return;
             for (int t = 1; t < kTeams; ++t) {
                 const float now = fmaxf(top, s_ml[t][0]);
-                const float a = top == -INFINITY ? 1.f : exp2f(top - now);
-                const float b = s_ml[t][0] == -INFINITY ? 1.f : exp2f(s_ml[t][0] - now);
+                const float a = top == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(top - now);
+                const float b =
+                    s_ml[t][0] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(s_ml[t][0] - now);
                 l = l * a + s_ml[t][1] * b;
                 sum = sum * a + s_o[t][threadIdx.x % kLanes] * b;
                 top = now;
@@ -1006,7 +1055,9 @@ int tile_rows(int max_rows, int group, int d) {
 }
 
 // Workgroups to cut the work for: what is resident at once.
-int target_items(int rows) { return device_cus() * (rows == 16 ? 4 : 2); }
+int target_items(int rows, int d) {
+    return device_cus() * (rows > 16 || d == 256 ? 2 : (d == 128 ? 3 : 4));
+}
 
 int64_t units_most(int n, int max_rows, int n_heads, int kv_heads, int rows) {
     const int64_t tiles = ((int64_t)max_rows * (n_heads / kv_heads) + rows - 1) / rows;
@@ -1027,9 +1078,9 @@ hipError_t launch_rows(const Args& g, hipStream_t st) {
     if (e != hipSuccess || !g.target) return e;
     const int tiles = (int)(units / g.c.heads / g.b.n);
     constexpr int RB = ROWS == 16 ? 1 : 16;
-    constexpr int kPer = RB == 1 ? 16 : ROWS / RB;
-    hipLaunchKernelGGL((kv_join_kernel<D, F16, ROWS, RB>), dim3((unsigned)(units * kPer)),
-                       dim3(kThreads), 0, st, g, tiles);
+    const int per_tile = ROWS == 16 ? g.b.max_rows * g.group : ROWS / RB;
+    hipLaunchKernelGGL((kv_join_kernel<D, F16, ROWS, RB>), dim3((unsigned)(units * per_tile)),
+                       dim3(kThreads), 0, st, g, tiles, per_tile);
     return hipGetLastError();
 }
 
@@ -1050,16 +1101,16 @@ int64_t kv_attention_blocks(int n, int max_rows, int n_heads, int kv_heads, int 
     const int rows = tile_rows(max_rows, n_heads / kv_heads, d);
     const int64_t units = units_most(n, max_rows, n_heads, kv_heads, rows);
     // Of the attention itself, and of the join (a workgroup for 1 or 16 rows).
-    return units * (rows == 16 ? 16 : rows / 16) + target_items(rows) + 8 * kXcdRun;
+    return units * (rows == 16 ? 16 : rows / 16) + target_items(rows, d) + 8 * kXcdRun;
 }
 
 size_t kv_attention_workspace_bytes(int n, int max_rows, int n_heads, int kv_heads, int d,
                                     int max_kv) {
-    if (max_kv <= kMinRun) return 0;
+    if (max_kv <= kWhole) return 0;
     const int rows = tile_rows(max_rows, n_heads / kv_heads, d);
-    const int64_t items = units_most(n, max_rows, n_heads, kv_heads, rows) + target_items(rows);
+    const int64_t items = units_most(n, max_rows, n_heads, kv_heads, rows) + target_items(rows, d);
     return align256((size_t)items * rows * d * sizeof(float)) +
-           align256((size_t)items * rows * sizeof(f32x2));
+           align256((size_t)items * rows * sizeof(f32x2)) + align256((size_t)n * sizeof(i32x4));
 }
 
 hipError_t launch_kv_attention(const KvCache& c, const KvBatch& b, const KvAttention& a,
@@ -1070,11 +1121,12 @@ hipError_t launch_kv_attention(const KvCache& c, const KvBatch& b, const KvAtten
     g.a = a;
     g.group = a.n_heads / c.heads;
     const int rows = tile_rows(b.max_rows, g.group, c.d);
-    g.target = a.max_kv > kMinRun ? target_items(rows) : 0;
+    g.target = a.max_kv > kWhole ? target_items(rows, c.d) : 0;
     const int64_t items = units_most(b.n, b.max_rows, a.n_heads, c.heads, rows) + g.target;
     g.part_o = (float*)workspace;
     g.part_ml =
         (f32x2*)((char*)workspace + align256((size_t)items * rows * c.d * sizeof(float)));
+    g.plans = (i32x4*)((char*)g.part_ml + align256((size_t)items * rows * sizeof(f32x2)));
     const bool f16 = a.dtype == DT_F16;
     if (c.d == 64) return f16 ? launch_d<64, true>(g, rows, st) : launch_d<64, false>(g, rows, st);
     if (c.d == 128)
