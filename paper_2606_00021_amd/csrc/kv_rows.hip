@@ -65,150 +65,186 @@ __device__ __forceinline__ void store8(void* p, int64_t at, const float* x) {
     }
 }
 
-// One thread's 8 values: which entry, layer, K or V, head and token.
+// A thread's token: which row of the tensors, and where in the cache.
 struct Place {
-    int64_t cell;    // rows in front in the cache, slot included
-    int64_t row;     // row of the tensor
-    int head, which, layer;
+    int64_t row;     // row of the tensors
+    int64_t page;    // page * rows of a page's K (or V, or head 0) ...
+    int slot;
+    int seq;
     bool ok;         // the token exists
     bool page_ok;
 };
 
-template <int D>
-__device__ __forceinline__ Place place(const KvCache& c, const KvBatch& b, const KvRows& r,
-                                       int lg_tokens, int blocks_per_entry, int token_tiles,
-                                       int* entry, int* seq) {
-    constexpr int kRows = kThreads / (D / 8);       // rows of a workgroup
-    const int row = threadIdx.x / (D / 8);
-    const int tokens = 1 << lg_tokens;              // token run of a workgroup
-    const int per = kRows >> lg_tokens;             // (K or V, head) pairs of a workgroup
-    const int i = blockIdx.x / blocks_per_entry;
-    const int rest = blockIdx.x % blocks_per_entry;
-    const int tile = rest % token_tiles;
-    const int pair = (rest / token_tiles) * per + (row >> lg_tokens);
-    const int j = tile * tokens + (row & (tokens - 1));
+// How a launch is cut: a workgroup has 2^lg tokens of one entry side by side
+// and `per` (K or V, head) pairs beside them, `loops` times.
+struct Shape {
+    int lg, tiles;       // tokens of a workgroup; workgroups along an entry's tokens
+    int per, loops;
+    int groups;          // workgroups along the pairs
+    int64_t blocks() const { return (int64_t)tiles * groups; }
+};
+
+__device__ __forceinline__ Place place(const KvCache& c, const KvBatch& b, int entry, int j) {
     Place p;
-    *entry = i;
-    const int s = kv_seq(c, b.seqs, i);
-    *seq = s;
-    p.layer = blockIdx.y;
-    p.which = pair >= c.heads;
-    p.head = pair - (p.which ? c.heads : 0);
-    p.ok = s >= 0 && pair < 2 * c.heads;
-    p.page_ok = false;
-    p.cell = p.row = 0;
-    if (!p.ok) return p;
-    const int m = kv_rows(b, i);
-    const int pos = kv_length(c, s) - m + j;
-    p.row = kv_start(b, i) + j;
+    p.row = 0;
+    p.page = 0;
+    p.slot = 0;
+    p.ok = p.page_ok = false;
+    p.seq = kv_seq(c, b.seqs, entry);
+    if (p.seq < 0) return p;
+    const int m = kv_rows(b, entry);
+    const int pos = kv_length(c, p.seq) - m + j;
+    p.row = kv_start(b, entry) + j;
     p.ok = j < m && pos >= 0 && p.row >= 0 && p.row < b.n_rows;
     if (!p.ok) return p;
-    const int id = c.page_table[(int64_t)s * c.max_pages + (pos >> c.lg_page)];
+    const int id = c.page_table[(int64_t)p.seq * c.max_pages + (pos >> c.lg_page)];
     p.page_ok = kv_page_ok(c, id);
-    if (p.page_ok)
-        p.cell = c.rows_before(r.layer + p.layer, id, p.which, p.head) + (pos & (c.page() - 1));
+    p.page = p.page_ok ? id : 0;
+    p.slot = pos & (c.page() - 1);
     return p;
 }
 
-// Bytes in front of block `blk` of the row at `cell`: scales lie block-major
-// in a page's head, so that neighbouring tokens' scales are neighbours.
-__device__ __forceinline__ int64_t scale_at(const KvCache& c, int64_t cell, int blk) {
-    const int64_t slot = cell & (c.page() - 1);
-    return (cell - slot) * (c.d / kKvBlock) + ((int64_t)blk << c.lg_page) + slot;
+// A workgroup's entry, first pair and token, from its number.
+struct Work {
+    int entry, pair, j;
+};
+template <int D>
+__device__ __forceinline__ Work work_of(const Shape& h) {
+    const int row = threadIdx.x / (D / 8);
+    const int at = blockIdx.x;
+    Work w;
+    const int blocks = h.tiles * h.groups;
+    w.entry = at / blocks;
+    const int rest = at % blocks;
+    w.j = (rest % h.tiles << h.lg) + (row & ((1 << h.lg) - 1));
+    w.pair = rest / h.tiles * h.per * h.loops + (row >> h.lg);
+    return w;
 }
+
+constexpr int kUnroll = 4;      // pairs whose bytes are on their way together
 
 template <int D, int DT>
 __global__ __launch_bounds__(kThreads) void kv_write_kernel(KvCache c, KvBatch b, KvRows r,
-                                                            int lg_tokens, int blocks_per_entry,
-                                                            int token_tiles) {
-    int i, s;
-    const Place p = place<D>(c, b, r, lg_tokens, blocks_per_entry, token_tiles, &i, &s);
+                                                            Shape h) {
+    const Work w = work_of<D>(h);
+    const Place p = place(c, b, w.entry, w.j);
+    const int vec = threadIdx.x % (D / 8);
     // A sequence that is listed again: its first entry is the one written.
     bool again = false;
     if (b.seqs) {
-        for (int t = threadIdx.x; t < i; t += kThreads) again |= b.seqs[t] == s;
+        for (int t = threadIdx.x; t < w.entry; t += kThreads) again |= b.seqs[t] == p.seq;
         again = __syncthreads_or(again);
     }
-    const int vec = threadIdx.x % (D / 8);
-    float x[8] = {};
-    const bool on = p.ok && p.page_ok && !again;
-    if (on)
-        load8<DT>(p.which ? r.v : r.k, p.layer * r.layer_stride + p.row * r.row_stride +
-                                           (int64_t)p.head * D + vec * 8, x);
-    uint32_t top = 0;
+    const int64_t from = blockIdx.y * r.layer_stride + p.row * r.row_stride + vec * 8;
+    for (int l0 = 0; l0 < h.loops; l0 += kUnroll) {
+        float x[kUnroll][8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const uint32_t u = __builtin_bit_cast(uint32_t, x[e]) & 0x7FFFFFFFu;
-        top = u > top ? u : top;
-    }
+        for (int u = 0; u < kUnroll; ++u) {
+            const int pair = w.pair + (l0 + u) * h.per;
+            const bool v = pair >= c.heads;
+            if (p.ok && l0 + u < h.loops && pair < 2 * c.heads) {
+                load8<DT>(v ? r.v : r.k, from + (int64_t)(pair - (v ? c.heads : 0)) * D, x[u]);
+            } else {
 #pragma unroll
-    for (int step = 1; step < 4; step <<= 1) {
-        const uint32_t o = (uint32_t)__shfl_xor((int)top, step);
-        top = o > top ? o : top;
+                for (int e = 0; e < 8; ++e) x[u][e] = 0.f;
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+            const int pair = w.pair + (l0 + u) * h.per;
+            uint32_t top = 0;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const uint32_t bits = __builtin_bit_cast(uint32_t, x[u][e]) & 0x7FFFFFFFu;
+                top = bits > top ? bits : top;
+            }
+#pragma unroll
+            for (int step = 1; step < 4; step <<= 1) {
+                const uint32_t o = (uint32_t)__shfl_xor((int)top, step);
+                top = o > top ? o : top;
+            }
+            if (!p.page_ok || again || l0 + u >= h.loops || pair >= 2 * c.heads) continue;
+            const bool finite = top < 0x7F800000u;
+            const int e = (int)(top >> 23) - 2;
+            const uint32_t sc = finite ? (uint32_t)(e > 0 ? e : 0) : 255u;
+            const float unit = __builtin_bit_cast(float, sc << 23);   // only its exponent is used
+            uint32_t code = 0;
+            code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, x[u][0], x[u][1], unit, 0);
+            code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, x[u][2], x[u][3], unit, 1);
+            code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, x[u][4], x[u][5], unit, 2);
+            code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, x[u][6], x[u][7], unit, 3);
+            // K and V pairs lie one after the other in a page.
+            const int64_t base =
+                c.rows_before(r.layer + (int)blockIdx.y, (int)p.page, 0, 0) + ((int64_t)pair << c.lg_page);
+            *(uint32_t*)(c.codes + (base + p.slot) * (D / 2) + vec * 4) = finite ? code : 0u;
+            if (vec % 4 == 0)
+                c.scales[base * (D / kKvBlock) + (vec / 4 << c.lg_page) + p.slot] = (uint8_t)sc;
+        }
     }
-    if (!on) return;
-    const bool finite = top < 0x7F800000u;
-    const int e = (int)(top >> 23) - 2;
-    const uint32_t sc = finite ? (uint32_t)(e > 0 ? e : 0) : 255u;
-    const float unit = __builtin_bit_cast(float, sc << 23);   // only its exponent is used
-    uint32_t w = 0;
-    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[0], x[1], unit, 0);
-    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[2], x[3], unit, 1);
-    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[4], x[5], unit, 2);
-    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[6], x[7], unit, 3);
-    *(uint32_t*)(c.codes + p.cell * (D / 2) + vec * 4) = finite ? w : 0u;
-    if (vec % 4 == 0) c.scales[scale_at(c, p.cell, vec / 4)] = (uint8_t)sc;
 }
 
 template <int D, int DT>
 __global__ __launch_bounds__(kThreads) void kv_read_kernel(KvCache c, KvBatch b, KvRows r,
-                                                           int lg_tokens, int blocks_per_entry,
-                                                           int token_tiles) {
-    int i, s;
-    const Place p = place<D>(c, b, r, lg_tokens, blocks_per_entry, token_tiles, &i, &s);
+                                                           Shape h) {
+    const Work w = work_of<D>(h);
+    const Place p = place(c, b, w.entry, w.j);
     if (!p.ok) return;
     const int vec = threadIdx.x % (D / 8);
-    float x[8] = {};
-    if (p.page_ok) {
-        const uint32_t w = *(const uint32_t*)(c.codes + p.cell * (D / 2) + vec * 4);
-        const float unit =
-            __builtin_bit_cast(float, (uint32_t)c.scales[scale_at(c, p.cell, vec / 4)] << 23);
-        const f32x2 a0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, unit, 0);
-        const f32x2 a1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, unit, 1);
-        const f32x2 a2 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, unit, 2);
-        const f32x2 a3 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, unit, 3);
-        x[0] = a0.x, x[1] = a0.y, x[2] = a1.x, x[3] = a1.y;
-        x[4] = a2.x, x[5] = a2.y, x[6] = a3.x, x[7] = a3.y;
+    const int64_t to = blockIdx.y * r.layer_stride + p.row * r.row_stride + vec * 8;
+    for (int l0 = 0; l0 < h.loops; l0 += kUnroll) {
+        uint32_t code[kUnroll], sc[kUnroll];
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+            const int pair = w.pair + (l0 + u) * h.per;
+            const bool on = l0 + u < h.loops && pair < 2 * c.heads;
+            const int64_t base = c.rows_before(r.layer + (int)blockIdx.y, (int)p.page, 0, 0) +
+                                 ((int64_t)(on ? pair : 0) << c.lg_page);
+            code[u] = *(const uint32_t*)(c.codes + (base + p.slot) * (D / 2) + vec * 4);
+            sc[u] = c.scales[base * (D / kKvBlock) + (vec / 4 << c.lg_page) + p.slot];
+        }
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+            const int pair = w.pair + (l0 + u) * h.per;
+            if (l0 + u >= h.loops || pair >= 2 * c.heads) continue;
+            const uint32_t x = p.page_ok ? code[u] : 0u;      // no page: zeros
+            const float unit = __builtin_bit_cast(float, (p.page_ok ? sc[u] : 0u) << 23);
+            const f32x2 a0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(x, unit, 0);
+            const f32x2 a1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(x, unit, 1);
+            const f32x2 a2 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(x, unit, 2);
+            const f32x2 a3 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(x, unit, 3);
+            const float y[8] = {a0.x, a0.y, a1.x, a1.y, a2.x, a2.y, a3.x, a3.y};
+            const bool v = pair >= c.heads;
+            store8<DT>(v ? r.v : r.k, to + (int64_t)(pair - (v ? c.heads : 0)) * D, y);
+        }
     }
-    store8<DT>(p.which ? r.v : r.k, p.layer * r.layer_stride + p.row * r.row_stride +
-                                        (int64_t)p.head * D + vec * 8, x);
 }
 
-// Token run (its logarithm), token runs of an entry, workgroups of an entry.
-struct Shape {
-    int lg, tiles, blocks;
-};
-Shape shape_of(const KvCache& c, const KvBatch& b) {
+Shape shape_of(const KvCache& c, const KvBatch& b, int n_layers) {
     const int rows = kThreads / (c.d / 8);
-    Shape s = {0, 0, 0};
+    Shape s;
+    s.lg = 0;
     while ((1 << s.lg) < b.max_rows && (1 << s.lg) < rows) ++s.lg;
     s.tiles = (b.max_rows + (1 << s.lg) - 1) >> s.lg;
-    const int per = rows >> s.lg;
-    s.blocks = (2 * c.heads + per - 1) / per * s.tiles;
+    s.per = rows >> s.lg;
+    const int pairs = (2 * c.heads + s.per - 1) / s.per;
+    // Workgroups take several pairs, so that a token's place is found once for
+    // them, while there are enough workgroups for the device.
+    const int64_t all = (int64_t)s.tiles * pairs * b.n * n_layers, enough = 4 * device_cus();
+    s.loops = 1;
+    while (s.loops < pairs && s.loops < 16 && all / (2 * s.loops) >= enough) s.loops *= 2;
+    s.groups = (pairs + s.loops - 1) / s.loops;
     return s;
 }
 
 template <bool WRITE, int D>
 hipError_t launch_d(const KvCache& c, const KvBatch& b, const KvRows& r, hipStream_t st) {
-    const Shape h = shape_of(c, b);
-    const dim3 grid((unsigned)((int64_t)h.blocks * b.n), (unsigned)r.n_layers);
-#define SENSE_KV_ROWS(T)                                                                     \
-    if constexpr (WRITE)                                                                     \
-        hipLaunchKernelGGL((kv_write_kernel<D, T>), grid, dim3(kThreads), 0, st, c, b, r,     \
-                           h.lg, h.blocks, h.tiles);                                         \
-    else                                                                                     \
-        hipLaunchKernelGGL((kv_read_kernel<D, T>), grid, dim3(kThreads), 0, st, c, b, r,      \
-                           h.lg, h.blocks, h.tiles)
+    const Shape h = shape_of(c, b, r.n_layers);
+    const dim3 grid((unsigned)(h.blocks() * b.n), (unsigned)r.n_layers);
+#define SENSE_KV_ROWS(T)                                                                      \
+    if constexpr (WRITE)                                                                      \
+        hipLaunchKernelGGL((kv_write_kernel<D, T>), grid, dim3(kThreads), 0, st, c, b, r, h); \
+    else                                                                                      \
+        hipLaunchKernelGGL((kv_read_kernel<D, T>), grid, dim3(kThreads), 0, st, c, b, r, h)
     if (r.dtype == DT_F32) {
         SENSE_KV_ROWS(DT_F32);
     } else if (r.dtype == DT_F16) {
@@ -230,7 +266,8 @@ hipError_t launch_rows(const KvCache& c, const KvBatch& b, const KvRows& r, hipS
 }  // namespace
 
 int64_t kv_rows_blocks(const KvCache& c, const KvBatch& b) {
-    return (int64_t)shape_of(c, b).blocks * b.n;
+    const Shape s = shape_of(c, b, 1);
+    return (int64_t)s.tiles * ((2 * c.heads + s.per - 1) / s.per) * b.n;
 }
 hipError_t launch_kv_write(const KvCache& c, const KvBatch& b, const KvRows& r, hipStream_t st) {
     return launch_rows<true>(c, b, r, st);

@@ -979,7 +979,8 @@ class _KvCall:
     def __init__(self, cache: dict, stream):
         dev = cache["codes"].device
         self.contexts = []
-        if dev.index != torch.cuda.current_device():
+        self.index = dev.index
+        if dev.index != torch._C._cuda_getDevice():
             self.contexts.append(torch.cuda.device(dev))
         if stream is not None:
             if not isinstance(stream, torch.cuda.Stream):
@@ -989,7 +990,7 @@ class _KvCall:
     def __enter__(self):
         for c in self.contexts:
             c.__enter__()
-        return _stream_handle(None)
+        return torch._C._cuda_getCurrentRawStream(self.index)
 
     def __exit__(self, *exc):
         for c in reversed(self.contexts):
