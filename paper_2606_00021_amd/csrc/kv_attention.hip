@@ -147,7 +147,10 @@ __device__ __forceinline__ Plan plan(const Args& g) {
     p.run = __builtin_amdgcn_readfirstlane(p.run);
     constexpr int kRun = ROWS <= 32 ? 1 : kXcdRun;
     const int idx = (int)(blockIdx.x >> 3);
-    const int item = ((idx / kRun) * 8 + (int)(blockIdx.x & 7)) * kRun + idx % kRun;
+    // The run of an XCD moves on by one each time, or a period of the items'
+    // sizes could give one XCD all the large ones.
+    const int turn = idx / kRun;
+    const int item = (turn * 8 + (int)((blockIdx.x + turn) & 7)) * kRun + idx % kRun;
     p.item = item;
     if (g.target && blockIdx.x == 0 && threadIdx.x < 64) {
         int at = upto - mine;
@@ -610,6 +613,21 @@ __global__ __launch_bounds__(kThreads, MT * D > 128 || MT == 2 ? 2 : (D == 128 ?
     }
 }
 
+// The tiles of a run of keys are items in this order: the last tiles first
+// (causal, they see the most keys), kXcdRun of a head side by side.
+__device__ __forceinline__ void tile_of(int at, int n_tiles, int heads, int* rt, int* head) {
+    const int block = at / (kXcdRun * heads), begin = block * kXcdRun;
+    const int wide = n_tiles - begin < kXcdRun ? n_tiles - begin : kXcdRun;
+    const int in = at - begin * heads;
+    *head = in / wide;
+    *rt = n_tiles - 1 - begin - in % wide;
+}
+__device__ __forceinline__ int place_of(int rt, int head, int n_tiles, int heads) {
+    const int back = n_tiles - 1 - rt, begin = back / kXcdRun * kXcdRun;
+    const int wide = n_tiles - begin < kXcdRun ? n_tiles - begin : kXcdRun;
+    return begin * heads + head * wide + back - begin;
+}
+
 // The same for many rows (draft trees, prompt chunks): a workgroup's four
 // waves have 16 MT rows each and share the keys.  A tile of KT keys is widened
 // once for all of them and laid into LDS in the order in which the matrix
@@ -637,9 +655,9 @@ __global__ __launch_bounds__(kThreads, 2) void kv_many_kernel(Args g) {
     const int col = lane & 15, grp = lane >> 4;
     const int n_tiles = (p.rows * g.group + kRows - 1) / kRows;
     const int local = p.item - p.first;
-    const int rt = n_tiles - 1 - local % n_tiles;       // tiles that see the most keys first
-    const int head = (local / n_tiles) % g.c.heads;
-    const int split = local / n_tiles / g.c.heads;
+    const int split = local / (n_tiles * g.c.heads);
+    int rt, head;
+    tile_of(local % (n_tiles * g.c.heads), n_tiles, g.c.heads, &rt, &head);
     const int r0 = rt * kRows;
     const int w0 = r0 + wave * 16 * MT;         // the wave's rows
     const int base = p.len - p.rows;
@@ -976,7 +994,8 @@ __global__ __launch_bounds__(kThreads) void kv_join_kernel(Args g, int tiles_max
     if (splits == 1) return;
     const int n_tiles = (rows * g.group + ROWS - 1) / ROWS;
     if (rt >= n_tiles) return;
-    const int place = ROWS <= 32 ? rt : n_tiles - 1 - rt;
+    const int place =
+        ROWS <= 32 ? head * n_tiles + rt : place_of(rt, head, n_tiles, g.c.heads);
     const int team = threadIdx.x / kLanes, dim = threadIdx.x % kLanes * 4;
     const int64_t start = kv_start(g.b, entry);
     for (int r = sub * RB + (RB == 1 ? 0 : team); r < (sub + 1) * RB; r += kTeams) {
@@ -990,7 +1009,7 @@ __global__ __launch_bounds__(kThreads) void kv_join_kernel(Args g, int tiles_max
             // The partial sums come from far (other XCDs wrote them): many at
             // a time; places behind the last read the first again, weight 0.
             constexpr int kEvery = RB == 1 ? kTeams : 1, kBatch = RB == 1 ? 16 : 8;
-            const int64_t first = ((int64_t)first_item + head * n_tiles + place) * ROWS + r;
+            const int64_t first = ((int64_t)first_item + place) * ROWS + r;
             const int64_t apart = (int64_t)g.c.heads * n_tiles * ROWS;
             for (int s0 = RB == 1 ? team : 0; s0 < splits; s0 += kBatch * kEvery) {
                 f32x2 ml[kBatch];
