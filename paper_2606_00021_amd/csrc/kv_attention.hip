@@ -640,13 +640,13 @@ __global__ __launch_bounds__(kThreads, 2) void kv_many_kernel(Args g) {
     constexpr int kRows = 64 * MT;
     constexpr int kKs = D / 32;
     constexpr int DV = D / 16;
-    constexpr int KT = D * MT >= 256 ? 32 : 64;     // keys of a tile
-    constexpr int kTiles = KT / 16;
-    constexpr int kSteps = KT / 32;
-    __shared__ u32x4 s_k[2][kTiles][kKs][64];
-    __shared__ u32x4 s_v[2][kSteps][DV][64];
-    __shared__ u32x4 s_nan[2][kSteps][64];  // 1 where a value is NaN
-    __shared__ int s_flag[2][kTiles];       // 1: no page, 2: some value is NaN
+    constexpr int KT = D == 256 ? 32 : 64;          // keys of a tile
+    constexpr int kTiles = D * MT >= 256 ? 2 : 4;   // 16 keys each, worked on at a time
+    constexpr int kSteps = kTiles / 2;
+    __shared__ u32x4 s_k[2][KT / 16][kKs][64];
+    __shared__ u32x4 s_v[2][KT / 32][DV][64];
+    __shared__ u32x4 s_nan[2][KT / 32][64]; // 1 where a value is NaN
+    __shared__ int s_flag[2][KT / 16];      // 1: no page, 2: some value is NaN
 
     const Plan p = plan<kRows>(g);
     if (p.entry < 0) return;
@@ -802,8 +802,9 @@ __global__ __launch_bounds__(kThreads, 2) void kv_many_kernel(Args g) {
         }
     };
 
-    // One tile.  plain: every row of the wave sees all of it, and its flags are 0.
-    auto compute = [&](int buf, int key, int flags, bool plain) {
+    // The 16-key parts of a tile from t0 on, `key` the first of their keys.
+    // plain: every row of the wave sees all of them, and their flags are 0.
+    auto compute = [&](int buf, int t0, int key, int flags, bool plain) {
         uint32_t vis[MT] = {};          // bit 4t + r: the row sees key 4 grp + r of quarter t
         if (!plain) {
 #pragma unroll
@@ -817,7 +818,7 @@ __global__ __launch_bounds__(kThreads, 2) void kv_many_kernel(Args g) {
 #pragma unroll
             for (int q = 0; q < kKs; ++q)
 #pragma unroll
-                for (int t = 0; t < kTiles; ++t) kf[q][t] = s_k[buf][t][q][lane];
+                for (int t = 0; t < kTiles; ++t) kf[q][t] = s_k[buf][t0 + t][q][lane];
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int q = 0; q < kKs; ++q)
@@ -880,12 +881,12 @@ __global__ __launch_bounds__(kThreads, 2) void kv_many_kernel(Args g) {
             constexpr int kBatch = DV < 8 ? DV : 8;
             u32x4 pf[MT];
 #pragma unroll
-            for (int t0 = 0; t0 < DV; t0 += kBatch) {
+            for (int d0 = 0; d0 < DV; d0 += kBatch) {
                 u32x4 vf[kBatch];
 #pragma unroll
-                for (int t = 0; t < kBatch; ++t) vf[t] = s_v[buf][step][t0 + t][lane];
+                for (int t = 0; t < kBatch; ++t) vf[t] = s_v[buf][t0 / 2 + step][d0 + t][lane];
                 __builtin_amdgcn_sched_barrier(0);
-                if (t0 == 0) {
+                if (d0 == 0) {
 #pragma unroll
                     for (int mt = 0; mt < MT; ++mt) {
 #pragma unroll
@@ -899,10 +900,10 @@ __global__ __launch_bounds__(kThreads, 2) void kv_many_kernel(Args g) {
                 for (int t = 0; t < kBatch; ++t)
 #pragma unroll
                     for (int mt = 0; mt < MT; ++mt)
-                        o[t0 + t][mt] = mfma<F16>(vf[t], pf[mt], o[t0 + t][mt]);
+                        o[d0 + t][mt] = mfma<F16>(vf[t], pf[mt], o[d0 + t][mt]);
             }
             if (flags & (0xA << (4 * step))) {
-                const u32x4 nan = s_nan[buf][step][lane];
+                const u32x4 nan = s_nan[buf][t0 / 2 + step][lane];
 #pragma unroll
                 for (int mt = 0; mt < MT; ++mt) {
                     const uint32_t v = vis[mt] >> (8 * step);
@@ -924,13 +925,18 @@ __global__ __launch_bounds__(kThreads, 2) void kv_many_kernel(Args g) {
         __syncthreads();
         int buf = 0;
         for (int key = key0; key < key1; key += KT) {
-            // Flags of the tile's quarters, two bits each.
+            // Flags of the tile's parts, two bits each.
             int flags = 0;
 #pragma unroll
-            for (int t = 0; t < kTiles; ++t) flags |= s_flag[buf][t] << (2 * t);
+            for (int t = 0; t < KT / 16; ++t) flags |= s_flag[buf][t] << (2 * t);
             flags = __builtin_amdgcn_readfirstlane(flags);
-            if (key < end)
-                compute(buf, key, flags, key + KT <= full && key + KT <= end && flags == 0);
+#pragma unroll
+            for (int t0 = 0; t0 < KT / 16; t0 += kTiles) {
+                const int at = key + 16 * t0, part = flags >> (2 * t0) & ((1 << 2 * kTiles) - 1);
+                if (at < end)
+                    compute(buf, t0, at, part, at + 16 * kTiles <= full && at + 16 * kTiles <= end &&
+                                                   part == 0);
+            }
             if (key + KT < key1) {
                 spread(buf ^ 1);
                 if (key + 2 * KT < key1) fetch(key + 2 * KT);
