@@ -636,12 +636,12 @@ __device__ __forceinline__ int place_of(int rt, int head, int n_tiles, int heads
 // keys (or their keys or values alone).  Each wave ends with whole rows, so
 // nothing is joined but runs.
 template <int D, bool F16, int MT>
-__global__ __launch_bounds__(kThreads, 2) void kv_many_kernel(Args g) {
+__global__ __launch_bounds__(kThreads, D >= 128 ? 2 : 3) void kv_many_kernel(Args g) {
     constexpr int kRows = 64 * MT;
     constexpr int kKs = D / 32;
     constexpr int DV = D / 16;
     constexpr int KT = D == 256 ? 32 : 64;          // keys of a tile
-    constexpr int kTiles = D * MT >= 256 ? 2 : 4;   // 16 keys each, worked on at a time
+    constexpr int kTiles = 2;                       // parts of 16 keys worked on at a time
     constexpr int kSteps = kTiles / 2;
     __shared__ u32x4 s_k[2][KT / 16][kKs][64];
     __shared__ u32x4 s_v[2][KT / 32][DV][64];
@@ -1081,6 +1081,7 @@ int tile_rows(int max_rows, int group, int d) {
 
 // Workgroups to cut the work for: what is resident at once.
 int target_items(int rows, int d) {
+    if (rows > 32) return device_cus() * (d >= 128 ? 2 : 3);
     return device_cus() * (rows > 16 || d == 256 ? 2 : (d == 128 ? 3 : 4));
 }
 
