@@ -87,10 +87,39 @@ struct Plan {
     int run;            // tiles of kTile keys in a run
 };
 
-__device__ __forceinline__ int64_t wave_sum64(int64_t v) {
-#pragma unroll
-    for (int s = 1; s < 64; s <<= 1) v += __shfl_xor((long long)v, s);
+// Inclusive prefix sums over a wave, in registers.
+__device__ __forceinline__ int wave_scan(int v) {
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false);     // row_shr:1
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);     // row_bcast:15
+    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);     // row_bcast:31
     return v;
+}
+__device__ __forceinline__ int wave_total(int v) {
+    return __builtin_amdgcn_readlane(wave_scan(v), 63);
+}
+
+// An entry's tiles of rows (of one head) and of keys.
+struct Size {
+    int seq, rows, len, units, tiles;
+};
+template <int ROWS>
+__device__ __forceinline__ Size size_of(const Args& g, int e) {
+    Size z = {kv_seq(g.c, g.b.seqs, e), 0, 0, 0, 0};
+    if (z.seq < 0) return z;
+    z.rows = kv_rows(g.b, e);
+    z.len = kv_length(g.c, z.seq);
+    z.units = (z.rows * g.group + ROWS - 1) / ROWS;
+    z.tiles = (z.len + kTile - 1) / kTile;
+    return z;
+}
+__device__ __forceinline__ int splits_of(int tiles, int run) {
+    return tiles > run ? (int)((unsigned)(tiles + run - 1) / (unsigned)run) : 1;
+}
+__device__ __forceinline__ int64_t divide(int64_t a, int b) {
+    return a >> 31 ? a / b : (int64_t)((unsigned)a / (unsigned)b);
 }
 
 // The items of the entries, in order, computed by every wave for itself from
@@ -101,50 +130,55 @@ __device__ __forceinline__ int64_t wave_sum64(int64_t v) {
 template <int ROWS>
 __device__ __forceinline__ Plan plan(const Args& g) {
     const int lane = threadIdx.x & 63;
+    // A lane has `per` entries from e0 on; the first is kept in registers (up
+    // to 64 entries are read once).
     const int n = g.b.n, per = (n + 63) / 64;
     const int e0 = lane * per < n ? lane * per : n;
     const int e1 = e0 + per < n ? e0 + per : n;
-    int64_t work = 0, whole = 0;
-    for (int e = e0; e < e1; ++e) {
-        const int s = kv_seq(g.c, g.b.seqs, e);
-        if (s < 0) continue;
-        const int m = kv_rows(g.b, e);
-        const int units = (m * g.group + ROWS - 1) / ROWS;
-        work += (int64_t)units * ((kv_length(g.c, s) + kTile - 1) / kTile);
-        whole += units;
+    Size z0 = {-1, 0, 0, 0, 0};
+    if (e0 < e1) z0 = size_of<ROWS>(g, e0);
+    int64_t work = (int64_t)z0.units * z0.tiles;
+    int units = z0.units;
+    for (int e = e0 + 1; e < e1; ++e) {
+        const Size z = size_of<ROWS>(g, e);
+        work += (int64_t)z.units * z.tiles;
+        units += z.units;
     }
-    work = wave_sum64(work) * g.c.heads;
-    whole = wave_sum64(whole) * g.c.heads;
-    int64_t run64 = g.target ? (work + g.target - 1) / g.target : 1 << 24;
+    // Fewer than 2^24 units of fewer than 2^24 tiles: two sums of 31 bits.
+    const int64_t all = ((int64_t)wave_total((int)(work >> 20)) << 20) +
+                        wave_total((int)(work & 0xFFFFF));
+    const int64_t whole = (int64_t)wave_total(units) * g.c.heads;
+    int64_t run64 = g.target ? divide(all * g.c.heads + g.target - 1, g.target) : 1 << 24;
     if (run64 < kMinRun / kTile) run64 = kMinRun / kTile;
-    Plan p;
-    p.run = __builtin_amdgcn_readfirstlane((int)(run64 < (1 << 24) ? run64 : (1 << 24)));
+    int run = __builtin_amdgcn_readfirstlane((int)(run64 < (1 << 24) ? run64 : (1 << 24)));
     // Items of the lane's entries with runs of that length.  Rounding up makes
     // more of them than `target`, and the last few would have the device to
     // themselves: the runs are made longer until they fit (or units are whole).
-    int mine, upto, total;
+    int mine, upto;
     for (int tries = 0;; ++tries) {
-        mine = 0;
-        for (int e = e0; e < e1; ++e) {
-            const int s = kv_seq(g.c, g.b.seqs, e);
-            if (s < 0) continue;
-            const int units = (kv_rows(g.b, e) * g.group + ROWS - 1) / ROWS;
-            const int tiles = (kv_length(g.c, s) + kTile - 1) / kTile;
-            const int splits = tiles > p.run ? (tiles + p.run - 1) / p.run : 1;
-            mine += units * splits * g.c.heads;
+        mine = z0.units * splits_of(z0.tiles, run);
+        for (int e = e0 + 1; e < e1; ++e) {
+            const Size z = size_of<ROWS>(g, e);
+            mine += z.units * splits_of(z.tiles, run);
         }
-        upto = mine;
-#pragma unroll
-        for (int s = 1; s < 64; s <<= 1) {
-            const int o = __shfl_up(upto, s);
-            if (lane >= s) upto += o;
-        }
-        total = __builtin_amdgcn_readlane(upto, 63);
+        mine *= g.c.heads;
+        upto = wave_scan(mine);
+        const int total = __builtin_amdgcn_readlane(upto, 63);
         if (total <= g.target || whole >= g.target || tries == kTries) break;
-        const int longer = (int)((int64_t)p.run * total / g.target);
-        p.run = __builtin_amdgcn_readfirstlane(longer > p.run ? longer : p.run + 1);
+        const int longer = (int)divide((int64_t)run * total, g.target);
+        run = __builtin_amdgcn_readfirstlane(longer > run ? longer : run + 1);
     }
-    p.run = __builtin_amdgcn_readfirstlane(p.run);
+    Plan p;
+    p.run = run;
+    if (g.target && blockIdx.x == 0 && threadIdx.x < 64) {
+        int at = upto - mine;
+        for (int e = e0; e < e1; ++e) {
+            const Size z = e == e0 ? z0 : size_of<ROWS>(g, e);
+            const int splits = splits_of(z.tiles, run);
+            g.plans[e] = i32x4{z.rows, at, splits, 0};
+            at += z.units * splits * g.c.heads;
+        }
+    }
     constexpr int kRun = ROWS <= 32 ? 1 : kXcdRun;
     const int idx = (int)(blockIdx.x >> 3);
     // The run of an XCD moves on by one each time, or a period of the items'
@@ -152,49 +186,34 @@ __device__ __forceinline__ Plan plan(const Args& g) {
     const int turn = idx / kRun;
     const int item = (turn * 8 + (int)((blockIdx.x + turn) & 7)) * kRun + idx % kRun;
     p.item = item;
-    if (g.target && blockIdx.x == 0 && threadIdx.x < 64) {
-        int at = upto - mine;
-        for (int e = e0; e < e1; ++e) {
-            const int s = kv_seq(g.c, g.b.seqs, e);
-            const int m = s < 0 ? 0 : kv_rows(g.b, e);
-            const int units = (m * g.group + ROWS - 1) / ROWS;
-            const int tiles = s < 0 ? 0 : (kv_length(g.c, s) + kTile - 1) / kTile;
-            const int splits = tiles > p.run ? (tiles + p.run - 1) / p.run : 1;
-            g.plans[e] = i32x4{m, at, splits, 0};
-            at += units * splits * g.c.heads;
-        }
-    }
-    const uint64_t who = __ballot(item >= upto - mine && item < upto);
     p.entry = -1;
-    p.seq = -1;
-    p.rows = p.len = p.first = 0;
-    p.splits = 1;
+    const uint64_t who = __ballot(item >= upto - mine && item < upto);
     if (!who) return p;
+    // The owner's chunk, walked by every lane alike.
     const int src = __builtin_ctzll(who);
-    // Walked by every lane alike: the owner's chunk.
+    int e = __builtin_amdgcn_readlane(e0, src);
     int at = __builtin_amdgcn_readlane(upto - mine, src);
-    const int c0 = __builtin_amdgcn_readlane(e0, src), c1 = __builtin_amdgcn_readlane(e1, src);
-    for (int e = c0; e < c1; ++e) {
-        const int s = kv_seq(g.c, g.b.seqs, e);
-        if (s < 0) continue;
-        const int m = kv_rows(g.b, e);
-        const int units = (m * g.group + ROWS - 1) / ROWS;
-        const int len = kv_length(g.c, s);
-        const int tiles = (len + kTile - 1) / kTile;
-        const int splits = tiles > p.run ? (tiles + p.run - 1) / p.run : 1;
-        const int mine_e = units * splits * g.c.heads;
-        if (item < at + mine_e) {
-            p.entry = __builtin_amdgcn_readfirstlane(e);
-            p.seq = __builtin_amdgcn_readfirstlane(s);
-            p.rows = __builtin_amdgcn_readfirstlane(m);
-            p.len = __builtin_amdgcn_readfirstlane(len);
+    Size z;
+    z.seq = __builtin_amdgcn_readlane(z0.seq, src);
+    z.rows = __builtin_amdgcn_readlane(z0.rows, src);
+    z.len = __builtin_amdgcn_readlane(z0.len, src);
+    z.units = __builtin_amdgcn_readlane(z0.units, src);
+    z.tiles = __builtin_amdgcn_readlane(z0.tiles, src);
+    for (;;) {
+        const int splits = splits_of(z.tiles, run);
+        const int next = at + z.units * splits * g.c.heads;
+        if (item < next || e + 1 >= n) {
+            p.entry = e;
+            p.seq = __builtin_amdgcn_readfirstlane(z.seq);
+            p.rows = __builtin_amdgcn_readfirstlane(z.rows);
+            p.len = __builtin_amdgcn_readfirstlane(z.len);
             p.first = __builtin_amdgcn_readfirstlane(at);
             p.splits = __builtin_amdgcn_readfirstlane(splits);
-            break;
+            return p;
         }
-        at += mine_e;
+        at = __builtin_amdgcn_readfirstlane(next);
+        z = size_of<ROWS>(g, ++e);
     }
-    return p;
 }
 
 template <bool F16>
@@ -309,12 +328,9 @@ __global__ __launch_bounds__(kThreads, MT * D > 128 || MT == 2 ? 2 : (D == 128 ?
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 15, grp = lane >> 4;
-    const int n_tiles = (p.rows * g.group + kRows - 1) / kRows;
     const int local = item - p.first;
-    const int rt = local % n_tiles;
-    const int head = (local / n_tiles) % g.c.heads;
-    const int split = local / n_tiles / g.c.heads;
-    const int r0 = rt * kRows;
+    const int split = local / g.c.heads, head = local - split * g.c.heads;
+    constexpr int r0 = 0;                       // a unit is one tile
     const int base = p.len - p.rows;            // position of the first new token
     const int64_t start = kv_start(g.b, p.entry);
 
