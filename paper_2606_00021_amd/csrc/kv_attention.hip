@@ -391,6 +391,8 @@ __global__ __launch_bounds__(kThreads, MT * D > 128 || MT == 2 ? 2 : (D == 128 ?
     const uint32_t ks_at = ((D == 64 ? grp >> 1 : (D == 128 ? grp : 2 * grp)) << lg) + col;
     const uint32_t vc_at = 4 * grp * (D / 2) + col * (D / 32);
     const uint32_t vs_at = ((col * DV / 32) << lg) + 4 * grp;
+    constexpr int kWide = D == 64 ? 2 : 4;      // words of a load
+    typedef uint32_t KeyBytes __attribute__((ext_vector_type(kWide)));
 
     auto pages = [&](int key) {
         Pages f;
@@ -414,7 +416,12 @@ __global__ __launch_bounds__(kThreads, MT * D > 128 || MT == 2 ? 2 : (D == 128 ?
             const uint8_t* ks = g.c.scales + kr * (D / 32) + slot;
             const uint8_t* vs = g.c.scales + vr * (D / 32) + slot;
 #pragma unroll
-            for (int w = 0; w < D / 32; ++w) f.k[t][w] = ((const uint32_t*)(kc + kc_at))[w];
+            for (int w = 0; w < D / 32; w += kWide) {
+                // Streamed: read once, they would push everything else out of L2.
+                const KeyBytes x = __builtin_nontemporal_load((const KeyBytes*)(kc + kc_at + 4 * w));
+#pragma unroll
+                for (int i = 0; i < kWide; ++i) f.k[t][w + i] = x[i];
+            }
 #pragma unroll
             for (int w = 0; w < (D == 256 ? 2 : 1); ++w) f.ks[t][w] = (ks + (w << lg))[ks_at];
 #pragma unroll
