@@ -951,50 +951,42 @@ def sense_build_kv_cache(n_layers: int, n_pages: int, page_size: int, n_kv_heads
 def _kv_desc(cache: dict) -> KvCacheDesc:
     codes, scales = cache["codes"], cache["scales"]
     table, lens, refs = cache["page_table"], cache["seq_len"], cache["page_refs"]
-    if codes.dim() != 6 or scales.dim() != 6 or table.dim() != 2:
-        raise ValueError("codes and scales must have 6 dimensions, page_table 2")
+    if codes.dim() != 6 or table.dim() != 2:
+        raise ValueError("codes must have 6 dimensions, page_table 2")
     layers, pages, two, heads, page, half = codes.shape
-    if two != 2 or tuple(scales.shape) != (layers, pages, 2, heads, half // 16, page):
+    seqs, max_pages = table.shape
+    if two != 2 or scales.shape != (layers, pages, 2, heads, half // 16, page):
         raise ValueError("codes are [layers, pages, 2, heads, page, d/2] and scales "
                          "[layers, pages, 2, heads, d/32, page]")
-    if lens.shape != (table.shape[0],) or refs.shape != (pages,):
+    if lens.shape != (seqs,) or refs.shape != (pages,):
         raise ValueError("seq_len has an entry a row of page_table, page_refs one a page")
+    if not (codes.dtype == scales.dtype == torch.uint8
+            and table.dtype == lens.dtype == refs.dtype == torch.int32):
+        raise ValueError("codes and scales are uint8, page_table, seq_len and page_refs int32")
     dev = codes.device
-    for t, dtype, name in ((codes, torch.uint8, "codes"), (scales, torch.uint8, "scales"),
-                           (table, torch.int32, "page_table"), (lens, torch.int32, "seq_len"),
-                           (refs, torch.int32, "page_refs")):
-        if t.dtype != dtype or not t.is_contiguous() or t.device != dev:
-            raise ValueError(f"{name} must be a contiguous {dtype} tensor on {dev}")
-    return KvCacheDesc(codes=_dev_ptr(codes, "codes"), scales=scales.data_ptr(),
-                       page_table=table.data_ptr(), seq_len=lens.data_ptr(),
-                       page_refs=refs.data_ptr(), n_layers=layers, n_pages=pages, page_size=page,
-                       n_kv_heads=heads, head_dim=2 * half, n_seqs=table.shape[0],
-                       max_pages=table.shape[1])
+    if not (codes.is_contiguous() and scales.is_contiguous() and table.is_contiguous()
+            and lens.is_contiguous() and refs.is_contiguous() and scales.device == dev
+            and table.device == dev and lens.device == dev and refs.device == dev):
+        raise ValueError(f"a cache's tensors must be contiguous and on one device ({dev})")
+    if not codes.is_cuda:
+        raise ValueError(f"a cache must be on a GPU (got {dev})")
+    return KvCacheDesc(codes.data_ptr(), scales.data_ptr(), table.data_ptr(), lens.data_ptr(),
+                       refs.data_ptr(), layers, pages, page, heads, 2 * half, seqs, max_pages)
 
 
-class _KvCall:
-    """A call on a cache: its device is made current and, where a stream is
+def _kv_on(cache: dict, stream, call):
+    """call(handle) with the cache's device current and, where a stream is
     named, that stream too, so that what is allocated inside belongs to it."""
-
-    def __init__(self, cache: dict, stream):
-        dev = cache["codes"].device
-        self.contexts = []
-        self.index = dev.index
-        if dev.index != torch._C._cuda_getDevice():
-            self.contexts.append(torch.cuda.device(dev))
-        if stream is not None:
-            if not isinstance(stream, torch.cuda.Stream):
-                stream = torch.cuda.ExternalStream(int(stream), device=dev)
-            self.contexts.append(torch.cuda.stream(stream))
-
-    def __enter__(self):
-        for c in self.contexts:
-            c.__enter__()
-        return torch._C._cuda_getCurrentRawStream(self.index)
-
-    def __exit__(self, *exc):
-        for c in reversed(self.contexts):
-            c.__exit__(*exc)
+    index = cache["codes"].device.index
+    if stream is None and index == torch._C._cuda_getDevice():
+        return call(torch._C._cuda_getCurrentRawStream(index))
+    with torch.cuda.device(index):
+        if stream is None:
+            return call(torch._C._cuda_getCurrentRawStream(index))
+        if not isinstance(stream, torch.cuda.Stream):
+            stream = torch.cuda.ExternalStream(int(stream), device=cache["codes"].device)
+        with torch.cuda.stream(stream):
+            return call(stream.cuda_stream)
 
 
 def _kv_scratch(cache: dict, workspace: torch.Tensor | None, size_call: str, *args):
@@ -1002,8 +994,7 @@ def _kv_scratch(cache: dict, workspace: torch.Tensor | None, size_call: str, *ar
     if workspace is None:
         size = ctypes.c_size_t()
         _check(getattr(load_library(), size_call)(*args, ctypes.byref(size)), size_call)
-        workspace = torch.empty(max(size.value, 1), dtype=torch.uint8,
-                                device=cache["codes"].device)
+        return cache["codes"].new_empty(max(size.value, 1))
     if workspace.dtype != torch.uint8 or not workspace.is_contiguous() \
             or workspace.device != cache["codes"].device:
         raise ValueError("workspace must be a contiguous uint8 tensor on the cache's device")
@@ -1076,10 +1067,9 @@ def _kv_rows(fn: str, cache: dict, layer: int, k: torch.Tensor, v: torch.Tensor,
     batch = _kv_batch(cache, tuple(k.shape[first:-2]), seqs, row_start, row_len, max_rows)
     if batch.n == 0 or batch.max_rows == 0 or layers == 0:
         return
-    with _KvCall(cache, stream) as st:
-        _check(getattr(load_library(), fn)(
-            ctypes.byref(desc), layer, layers, k.data_ptr(), v.data_ptr(), _TORCH_DTYPE[k.dtype],
-            row, layer_stride, ctypes.byref(batch), st), fn)
+    _kv_on(cache, stream, lambda st: _check(getattr(load_library(), fn)(
+        ctypes.byref(desc), layer, layers, k.data_ptr(), v.data_ptr(), _TORCH_DTYPE[k.dtype],
+        row, layer_stride, ctypes.byref(batch), st), fn))
 
 
 def sense_kv_write(cache: dict, layer: int, k: torch.Tensor, v: torch.Tensor,
@@ -1150,25 +1140,27 @@ def sense_kv_attention(cache: dict, layer: int, q: torch.Tensor, mask: torch.Ten
         ld = mask.stride(1) if mask.shape[1] > 1 else mask.shape[2]
         step = mask.stride(0)
     heads = q.shape[-2]
-    with _KvCall(cache, stream) as st:
-        if out is None:
-            out = torch.empty(q.shape, dtype=q.dtype, device=dev)
+
+    def call(st):
+        o = torch.empty_like(q, memory_format=torch.contiguous_format) if out is None else out
         if batch.n == 0 or batch.max_rows == 0:
-            return out
-        workspace = _kv_scratch(cache, workspace, "sense_kv_attention_workspace_size",
-                                ctypes.byref(desc), batch.n, batch.max_rows, heads, max_kv)
+            return o
+        ws = _kv_scratch(cache, workspace, "sense_kv_attention_workspace_size",
+                         ctypes.byref(desc), batch.n, batch.max_rows, heads, max_kv)
         _check(load_library().sense_kv_attention(
             ctypes.byref(desc), layer, q.data_ptr(), _TORCH_DTYPE[q.dtype], heads,
             _kv_row_stride(q, 0, "q"), ctypes.byref(batch),
             None if mask is None else mask.data_ptr(), ld, step,
             q.shape[-1] ** -0.5 if softmax_scale is None else softmax_scale, max_kv,
-            out.data_ptr(), _kv_row_stride(out, 0, "out"), workspace.data_ptr(),
-            workspace.numel(), st), "sense_kv_attention")
-    return out
+            o.data_ptr(), _kv_row_stride(o, 0, "out"), ws.data_ptr(), ws.numel(), st),
+            "sense_kv_attention")
+        return o
+
+    return _kv_on(cache, stream, call)
 
 
 def _kv_status(cache: dict, n: int) -> torch.Tensor:
-    return torch.empty(n, dtype=torch.int32, device=cache["codes"].device)
+    return cache["seq_len"].new_empty(n)
 
 
 def sense_kv_truncate(cache: dict, lens: torch.Tensor | None = None,
@@ -1177,12 +1169,15 @@ def sense_kv_truncate(cache: dict, lens: torch.Tensor | None = None,
     without it: the sequences are freed); returns an int32 status each."""
     desc = _kv_desc(cache)
     n = (seqs.numel() if seqs is not None else lens.numel() if lens is not None else desc.n_seqs)
-    with _KvCall(cache, stream) as st:
+
+    def call(st):
         status = _kv_status(cache, n)
         _check(load_library().sense_kv_truncate(
             ctypes.byref(desc), _kv_ints(seqs, n, cache, "seqs"),
             _kv_ints(lens, n, cache, "lens"), n, status.data_ptr(), st), "sense_kv_truncate")
-    return status
+        return status
+
+    return _kv_on(cache, stream, call)
 
 
 def sense_kv_fork(cache: dict, src: torch.Tensor, dst: torch.Tensor, stream=None) -> torch.Tensor:
@@ -1190,12 +1185,15 @@ def sense_kv_fork(cache: dict, src: torch.Tensor, dst: torch.Tensor, stream=None
     int32 status each."""
     desc = _kv_desc(cache)
     n = src.numel()
-    with _KvCall(cache, stream) as st:
+
+    def call(st):
         status = _kv_status(cache, n)
         _check(load_library().sense_kv_fork(
             ctypes.byref(desc), _kv_ints(src, n, cache, "src"), _kv_ints(dst, n, cache, "dst"), n,
             status.data_ptr(), st), "sense_kv_fork")
-    return status
+        return status
+
+    return _kv_on(cache, stream, call)
 
 
 def sense_kv_reserve(cache: dict, counts: torch.Tensor, seqs: torch.Tensor | None = None,
@@ -1204,15 +1202,18 @@ def sense_kv_reserve(cache: dict, counts: torch.Tensor, seqs: torch.Tensor | Non
     copying a shared last page first; returns an int32 status each."""
     desc = _kv_desc(cache)
     n = counts.numel()
-    with _KvCall(cache, stream) as st:
+
+    def call(st):
         status = _kv_status(cache, n)
-        workspace = _kv_scratch(cache, workspace, "sense_kv_reserve_workspace_size",
-                                ctypes.byref(desc), n)
+        ws = _kv_scratch(cache, workspace, "sense_kv_reserve_workspace_size",
+                         ctypes.byref(desc), n)
         _check(load_library().sense_kv_reserve(
             ctypes.byref(desc), _kv_ints(seqs, n, cache, "seqs"),
             _kv_ints(counts, n, cache, "counts"), n, status.data_ptr(),
-            workspace.data_ptr(), workspace.numel(), st), "sense_kv_reserve")
-    return status
+            ws.data_ptr(), ws.numel(), st), "sense_kv_reserve")
+        return status
+
+    return _kv_on(cache, stream, call)
 
 
 def sense_kv_compact(cache: dict, tails: torch.Tensor, keep: torch.Tensor,
@@ -1232,14 +1233,16 @@ def sense_kv_compact(cache: dict, tails: torch.Tensor, keep: torch.Tensor,
         raise ValueError("keep must be [n, ld] or [n * rows, ld]")
     if rows > 1 and pick is None:
         raise ValueError("pick must name the row of each entry")
-    with _KvCall(cache, stream) as st:
+
+    def call(st):
         status = _kv_status(cache, n)
-        workspace = _kv_scratch(cache, workspace, "sense_kv_compact_workspace_size", n,
-                                keep.shape[-1])
+        ws = _kv_scratch(cache, workspace, "sense_kv_compact_workspace_size", n, keep.shape[-1])
         _check(load_library().sense_kv_compact(
             ctypes.byref(desc), _kv_ints(seqs, n, cache, "seqs"),
             _kv_ints(tails, n, cache, "tails"), _kv_ints(keep, None, cache, "keep"),
             _kv_ints(keep_len, n * rows, cache, "keep_len"), _kv_ints(pick, n, cache, "pick"),
             max(rows, 1), keep.shape[-1], n, status.data_ptr(),
-            workspace.data_ptr(), workspace.numel(), st), "sense_kv_compact")
-    return status
+            ws.data_ptr(), ws.numel(), st), "sense_kv_compact")
+        return status
+
+    return _kv_on(cache, stream, call)

@@ -105,7 +105,7 @@ def test_bad_rows(lib, kw, status):
     (dict(mask=FAKE, mask_ld=3), INVALID), (dict(mask=FAKE, mask_ld=4, mask_stride=-1), INVALID),
     (dict(q=None), INVALID), (dict(out=None), INVALID), (dict(q_stride=255), INVALID),
     (dict(q_stride=257), MISALIGNED), (dict(q=FAKE + 4), MISALIGNED), (dict(out=FAKE + 8), MISALIGNED),
-    (dict(out_stride=260), MISALIGNED), (dict(ws=None, max_kv=1000, pages=1000), WORKSPACE),
+    (dict(out_stride=260), MISALIGNED), (dict(ws=None, max_kv=2000, pages=1000), WORKSPACE),
     (dict(ws_bytes=64, pages=1000), WORKSPACE), (dict(ws=FAKE + 16, pages=1000), MISALIGNED),
 ])
 def test_bad_attention(lib, kw, status):
