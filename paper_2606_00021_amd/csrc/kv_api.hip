@@ -352,7 +352,7 @@ SENSE_EXPORT sense_status_t sense_kv_compact(const sense_kv_cache_t* cache, cons
     if (n == 0) return ok();
     if (!tails || !keep || !keep_len)
         return fail(SENSE_ERR_INVALID_ARGUMENT, "tails, keep and keep_len must be non-NULL");
-    if ((int64_t)n * c.n_layers * 2 * c.heads / 4 > kMaxBlocks)
+    if ((int64_t)n * (1 + (int64_t)c.n_layers * 2 * c.heads) / 4 > kMaxBlocks)
         return fail(SENSE_ERR_UNSUPPORTED, "%d entries of %d layers: too many for one call", n,
                     c.n_layers);
     if ((s = check_workspace(workspace, workspace_bytes,

@@ -74,7 +74,7 @@ struct Args {
     int target;         // workgroups that the work is cut for (0: units stay whole)
     float* part_o;      // [item][rows][d]
     f32x2* part_ml;     // [item][rows]: reference, sum
-    i32x4* plans;       // [entry]: new tokens, first item, runs of a unit
+    i32x4* plans;       // [entry]: new tokens, first item, runs of a unit, tiles of a run
 };
 
 // Where one unit tile's items lie, and which keys one of them has.
@@ -122,28 +122,29 @@ __device__ __forceinline__ int64_t divide(int64_t a, int b) {
     return a >> 31 ? a / b : (int64_t)((unsigned)a / (unsigned)b);
 }
 
-// The items of the entries, in order, computed by every wave for itself from
-// the entries' lengths, and the one of this workgroup.  Workgroups are dealt
-// to the 8 XCDs in turn; items go to them in short runs, so that tiles which
-// read the same keys share an L2 and every XCD still has its part of each
-// entry.  The first workgroup leaves the entries' items for the join.
+// The item of this workgroup.  Workgroups are dealt to the 8 XCDs in turn;
+// items go to them in short runs, so that tiles which read the same keys share
+// an L2 and every XCD still has its part of each entry.
 template <int ROWS>
-__device__ __forceinline__ Plan plan(const Args& g) {
+__device__ __forceinline__ int item_of_block() {
+    constexpr int kRun = ROWS <= 32 ? 1 : kXcdRun;
+    const int idx = (int)(blockIdx.x >> 3);
+    // The run of an XCD moves on by one each time, or a period of the items'
+    // sizes could give one XCD all the large ones.
+    const int turn = idx / kRun;
+    return (turn * 8 + (int)((blockIdx.x + turn) & 7)) * kRun + idx % kRun;
+}
+
+// The items of up to 64 entries, in order, computed by every wave for itself
+// from the entries' lengths, a lane an entry.  The first workgroup leaves them
+// for the join.
+template <int ROWS>
+__device__ __forceinline__ Plan plan_few(const Args& g) {
     const int lane = threadIdx.x & 63;
-    // A lane has `per` entries from e0 on; the first is kept in registers (up
-    // to 64 entries are read once).
-    const int n = g.b.n, per = (n + 63) / 64;
-    const int e0 = lane * per < n ? lane * per : n;
-    const int e1 = e0 + per < n ? e0 + per : n;
     Size z0 = {-1, 0, 0, 0, 0};
-    if (e0 < e1) z0 = size_of<ROWS>(g, e0);
-    int64_t work = (int64_t)z0.units * z0.tiles;
-    int units = z0.units;
-    for (int e = e0 + 1; e < e1; ++e) {
-        const Size z = size_of<ROWS>(g, e);
-        work += (int64_t)z.units * z.tiles;
-        units += z.units;
-    }
+    if (lane < g.b.n) z0 = size_of<ROWS>(g, lane);
+    const int64_t work = (int64_t)z0.units * z0.tiles;
+    const int units = z0.units;
     // Fewer than 2^24 units of fewer than 2^24 tiles: two sums of 31 bits.
     const int64_t all = ((int64_t)wave_total((int)(work >> 20)) << 20) +
                         wave_total((int)(work & 0xFFFFF));
@@ -151,69 +152,134 @@ __device__ __forceinline__ Plan plan(const Args& g) {
     int64_t run64 = g.target ? divide(all * g.c.heads + g.target - 1, g.target) : 1 << 24;
     if (run64 < kMinRun / kTile) run64 = kMinRun / kTile;
     int run = __builtin_amdgcn_readfirstlane((int)(run64 < (1 << 24) ? run64 : (1 << 24)));
-    // Items of the lane's entries with runs of that length.  Rounding up makes
+    // Items of the lane's entry with runs of that length.  Rounding up makes
     // more of them than `target`, and the last few would have the device to
     // themselves: the runs are made longer until they fit (or units are whole).
     int mine, upto;
     for (int tries = 0;; ++tries) {
-        mine = z0.units * splits_of(z0.tiles, run);
-        for (int e = e0 + 1; e < e1; ++e) {
-            const Size z = size_of<ROWS>(g, e);
-            mine += z.units * splits_of(z.tiles, run);
-        }
-        mine *= g.c.heads;
+        mine = z0.units * splits_of(z0.tiles, run) * g.c.heads;
         upto = wave_scan(mine);
         const int total = __builtin_amdgcn_readlane(upto, 63);
         if (total <= g.target || whole >= g.target || tries == kTries) break;
         const int longer = (int)divide((int64_t)run * total, g.target);
         run = __builtin_amdgcn_readfirstlane(longer > run ? longer : run + 1);
     }
+    if (g.target && blockIdx.x == 0 && threadIdx.x < g.b.n)
+        g.plans[threadIdx.x] = i32x4{z0.rows, upto - mine, splits_of(z0.tiles, run), run};
     Plan p;
-    p.run = run;
-    if (g.target && blockIdx.x == 0 && threadIdx.x < 64) {
-        int at = upto - mine;
-        for (int e = e0; e < e1; ++e) {
-            const Size z = e == e0 ? z0 : size_of<ROWS>(g, e);
-            const int splits = splits_of(z.tiles, run);
-            g.plans[e] = i32x4{z.rows, at, splits, 0};
-            at += z.units * splits * g.c.heads;
-        }
-    }
-    constexpr int kRun = ROWS <= 32 ? 1 : kXcdRun;
-    const int idx = (int)(blockIdx.x >> 3);
-    // The run of an XCD moves on by one each time, or a period of the items'
-    // sizes could give one XCD all the large ones.
-    const int turn = idx / kRun;
-    const int item = (turn * 8 + (int)((blockIdx.x + turn) & 7)) * kRun + idx % kRun;
-    p.item = item;
+    p.item = item_of_block<ROWS>();
     p.entry = -1;
-    const uint64_t who = __ballot(item >= upto - mine && item < upto);
+    const uint64_t who = __ballot(p.item >= upto - mine && p.item < upto);
     if (!who) return p;
-    // The owner's chunk, walked by every lane alike.
     const int src = __builtin_ctzll(who);
-    int e = __builtin_amdgcn_readlane(e0, src);
-    int at = __builtin_amdgcn_readlane(upto - mine, src);
-    Size z;
-    z.seq = __builtin_amdgcn_readlane(z0.seq, src);
-    z.rows = __builtin_amdgcn_readlane(z0.rows, src);
-    z.len = __builtin_amdgcn_readlane(z0.len, src);
-    z.units = __builtin_amdgcn_readlane(z0.units, src);
-    z.tiles = __builtin_amdgcn_readlane(z0.tiles, src);
-    for (;;) {
-        const int splits = splits_of(z.tiles, run);
-        const int next = at + z.units * splits * g.c.heads;
-        if (item < next || e + 1 >= n) {
-            p.entry = e;
-            p.seq = __builtin_amdgcn_readfirstlane(z.seq);
-            p.rows = __builtin_amdgcn_readfirstlane(z.rows);
-            p.len = __builtin_amdgcn_readfirstlane(z.len);
-            p.first = __builtin_amdgcn_readfirstlane(at);
-            p.splits = __builtin_amdgcn_readfirstlane(splits);
-            return p;
-        }
-        at = __builtin_amdgcn_readfirstlane(next);
-        z = size_of<ROWS>(g, ++e);
+    p.entry = src;
+    p.seq = __builtin_amdgcn_readlane(z0.seq, src);
+    p.rows = __builtin_amdgcn_readlane(z0.rows, src);
+    p.len = __builtin_amdgcn_readlane(z0.len, src);
+    p.first = __builtin_amdgcn_readlane(upto - mine, src);
+    p.run = run;
+    p.splits = __builtin_amdgcn_readfirstlane(
+        splits_of(__builtin_amdgcn_readlane(z0.tiles, src), run));
+    return p;
+}
+
+// The same for more entries, by one workgroup in front of the attention.
+constexpr int kPlanThreads = 1024;
+__device__ __forceinline__ int64_t block_scan(int64_t v, int64_t* s_wave, int64_t* total) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+    for (int s = 1; s < 64; s <<= 1) {
+        const int64_t o = __shfl_up((long long)v, s);
+        if (lane >= s) v += o;
     }
+    if (lane == 63) s_wave[wave] = v;
+    __syncthreads();
+    int64_t before = 0, all = 0;
+    for (int w = 0; w < kPlanThreads / 64; ++w) {
+        if (w < wave) before += s_wave[w];
+        all += s_wave[w];
+    }
+    __syncthreads();
+    *total = all;
+    return v + before;
+}
+
+template <int ROWS>
+__global__ __launch_bounds__(kPlanThreads) void kv_plan_kernel(Args g) {
+    __shared__ int64_t s_wave[kPlanThreads / 64];
+    int64_t work = 0, units = 0, all, whole;
+    for (int e = threadIdx.x; e < g.b.n; e += kPlanThreads) {
+        const Size z = size_of<ROWS>(g, e);
+        work += (int64_t)z.units * z.tiles;
+        units += z.units;
+    }
+    block_scan(work, s_wave, &all);
+    block_scan(units, s_wave, &whole);
+    whole *= g.c.heads;
+    int64_t run64 = g.target ? divide(all * g.c.heads + g.target - 1, g.target) : 1 << 24;
+    if (run64 < kMinRun / kTile) run64 = kMinRun / kTile;
+    int run = (int)(run64 < (1 << 24) ? run64 : (1 << 24));
+    for (int tries = 0; whole < g.target && tries < kTries; ++tries) {
+        int64_t mine = 0, total;
+        for (int e = threadIdx.x; e < g.b.n; e += kPlanThreads) {
+            const Size z = size_of<ROWS>(g, e);
+            mine += z.units * splits_of(z.tiles, run);
+        }
+        block_scan(mine, s_wave, &total);
+        total *= g.c.heads;
+        if (total <= g.target) break;
+        const int longer = (int)divide((int64_t)run * total, g.target);
+        run = longer > run ? longer : run + 1;
+    }
+    int64_t at = 0;
+    for (int e0 = 0; e0 < g.b.n; e0 += kPlanThreads) {
+        const int e = e0 + threadIdx.x;
+        Size z = {-1, 0, 0, 0, 0};
+        if (e < g.b.n) z = size_of<ROWS>(g, e);
+        const int splits = splits_of(z.tiles, run);
+        const int64_t mine = (int64_t)z.units * splits * g.c.heads;
+        int64_t total;
+        const int64_t upto = block_scan(mine, s_wave, &total);
+        if (e < g.b.n) g.plans[e] = i32x4{z.rows, (int)(at + upto - mine), splits, run};
+        at += total;
+    }
+    if (threadIdx.x == 0) g.plans[g.b.n] = i32x4{0, (int)at, 1, run};
+}
+
+// This workgroup's item in that plan: the last entry whose first item is not
+// behind it (entries without items share theirs with the next), 64 at a time.
+template <int ROWS>
+__device__ __forceinline__ Plan plan_many(const Args& g) {
+    const int lane = threadIdx.x & 63;
+    Plan p;
+    p.item = item_of_block<ROWS>();
+    p.entry = -1;
+    int from = 0, to = g.b.n + 1;               // the one behind the last holds the total
+    while (to - from > 1) {
+        const int step = (to - from + 63) / 64;
+        const int e = from + lane * step;
+        const uint64_t not_behind = __ballot(e < to && g.plans[e < to ? e : from][1] <= p.item);
+        // The first is never behind: bit 0 is set.
+        const int last = 63 - __builtin_clzll(not_behind);
+        to = from + (last + 1) * step < to ? from + (last + 1) * step : to;
+        from = from + last * step;
+    }
+    if (from == g.b.n) return p;
+    const Size z = size_of<ROWS>(g, from);
+    p.entry = from;
+    p.seq = __builtin_amdgcn_readfirstlane(z.seq);
+    p.rows = __builtin_amdgcn_readfirstlane(z.rows);
+    p.len = __builtin_amdgcn_readfirstlane(z.len);
+    const i32x4 x = g.plans[from];
+    p.first = __builtin_amdgcn_readfirstlane(x[1]);
+    p.splits = __builtin_amdgcn_readfirstlane(x[2]);
+    p.run = __builtin_amdgcn_readfirstlane(x[3]);
+    return p;
+}
+
+template <int ROWS>
+__device__ __forceinline__ Plan plan(const Args& g) {
+    return g.b.n <= 64 ? plan_few<ROWS>(g) : plan_many<ROWS>(g);
 }
 
 template <bool F16>
@@ -1116,6 +1182,11 @@ int64_t units_most(int n, int max_rows, int n_heads, int kv_heads, int rows) {
 template <int D, bool F16, int ROWS>
 hipError_t launch_rows(const Args& g, hipStream_t st) {
     const int64_t units = units_most(g.b.n, g.b.max_rows, g.a.n_heads, g.c.heads, ROWS);
+    if (g.b.n > 64) {
+        hipLaunchKernelGGL((kv_plan_kernel<ROWS>), dim3(1), dim3(kPlanThreads), 0, st, g);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
     // Whole runs for every XCD; at most target + units items.
     const int64_t per = ROWS <= 32 ? 8 : 8 * kXcdRun;
     const dim3 grid((unsigned)((units + g.target + per - 1) / per * per));
@@ -1153,13 +1224,27 @@ int64_t kv_attention_blocks(int n, int max_rows, int n_heads, int kv_heads, int 
     return units * (rows == 16 ? 16 : rows / 16) + target_items(rows, d) + 8 * kXcdRun;
 }
 
+// Partial sums, where units may be cut, and the entries' plans.
+struct Layout {
+    int rows, target;
+    size_t ml, plans, total;
+};
+Layout layout_of(int n, int max_rows, int n_heads, int kv_heads, int d, int max_kv) {
+    Layout l;
+    l.rows = tile_rows(max_rows, n_heads / kv_heads, d);
+    l.target = max_kv > kWhole ? target_items(l.rows, d) : 0;
+    const size_t rows =
+        l.target ? (size_t)(units_most(n, max_rows, n_heads, kv_heads, l.rows) + l.target) * l.rows
+                 : 0;
+    l.ml = align256(rows * d * sizeof(float));
+    l.plans = l.ml + align256(rows * sizeof(f32x2));
+    l.total = l.plans + (l.target || n > 64 ? align256((size_t)(n + 1) * sizeof(i32x4)) : 0);
+    return l;
+}
+
 size_t kv_attention_workspace_bytes(int n, int max_rows, int n_heads, int kv_heads, int d,
                                     int max_kv) {
-    if (max_kv <= kWhole) return 0;
-    const int rows = tile_rows(max_rows, n_heads / kv_heads, d);
-    const int64_t items = units_most(n, max_rows, n_heads, kv_heads, rows) + target_items(rows, d);
-    return align256((size_t)items * rows * d * sizeof(float)) +
-           align256((size_t)items * rows * sizeof(f32x2)) + align256((size_t)n * sizeof(i32x4));
+    return layout_of(n, max_rows, n_heads, kv_heads, d, max_kv).total;
 }
 
 hipError_t launch_kv_attention(const KvCache& c, const KvBatch& b, const KvAttention& a,
@@ -1169,13 +1254,12 @@ hipError_t launch_kv_attention(const KvCache& c, const KvBatch& b, const KvAtten
     g.b = b;
     g.a = a;
     g.group = a.n_heads / c.heads;
-    const int rows = tile_rows(b.max_rows, g.group, c.d);
-    g.target = a.max_kv > kWhole ? target_items(rows, c.d) : 0;
-    const int64_t items = units_most(b.n, b.max_rows, a.n_heads, c.heads, rows) + g.target;
+    const Layout l = layout_of(b.n, b.max_rows, a.n_heads, c.heads, c.d, a.max_kv);
+    const int rows = l.rows;
+    g.target = l.target;
     g.part_o = (float*)workspace;
-    g.part_ml =
-        (f32x2*)((char*)workspace + align256((size_t)items * rows * c.d * sizeof(float)));
-    g.plans = (i32x4*)((char*)g.part_ml + align256((size_t)items * rows * sizeof(f32x2)));
+    g.part_ml = (f32x2*)((char*)workspace + l.ml);
+    g.plans = (i32x4*)((char*)workspace + l.plans);
     const bool f16 = a.dtype == DT_F16;
     if (c.d == 64) return f16 ? launch_d<64, true>(g, rows, st) : launch_d<64, false>(g, rows, st);
     if (c.d == 128)

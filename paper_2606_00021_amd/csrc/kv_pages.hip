@@ -7,8 +7,8 @@
 // numbers, entries are served in order of the list.  What an operation has to
 // move is small (tables, one page a sequence, a path of some tokens a layer),
 // so these kernels are bound by launches and by the latency of dependent
-// loads: one plan by a single workgroup where entries depend on each other,
-// then one launch over all layers for the bytes.
+// loads: one launch that decides (a single workgroup where entries depend on
+// each other), then one over all layers for the bytes.
 #include "internal.h"
 #include "kv.h"
 
@@ -289,8 +289,8 @@ __global__ __launch_bounds__(kThreads) void kv_copy_kernel(KvCache c, const Copy
 
 // ---------------------------------------------------------------- compact
 
-// Workspace: per entry the number of rows to move, then the moves themselves
-// (cache rows of layer 0's K, head 0: page * page size + slot) as pairs.
+// Workspace: per entry the length to cut to (-1: refused), the number of rows
+// to move, then the moves themselves (page * page size + slot) as pairs.
 struct Move {
     int64_t src, dst;
 };
@@ -301,64 +301,47 @@ __device__ __forceinline__ int64_t cell_of(const KvCache& c, int s, int pos) {
     return ((int64_t)id << c.lg_page) + (pos & (c.page() - 1));
 }
 
-// One workgroup.  First every entry is judged and its moves are written down
-// from the table as it was, a wave an entry; then lengths are cut and pages
-// released.
-__global__ __launch_bounds__(kPlanThreads) void kv_compact_kernel(KvCache c, const int32_t* seqs,
-                                                                  KvKeep k, int n,
-                                                                  int32_t* status, int32_t* count,
-                                                                  Move* moves) {
-    __shared__ int s_seq[kKvMaxEntries];
-    __shared__ int s_end[kKvMaxEntries];     // length to cut to, or -1
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    for (int i = threadIdx.x; i < n; i += kPlanThreads) s_seq[i] = kv_seq(c, seqs, i);
-    __syncthreads();
-    for (int i = wave; i < n; i += kPlanThreads / 64) {
-        const int s = s_seq[i], tail = k.tails[i];
-        const int pick = k.pick ? k.pick[i] : 0;
-        bool bad = s < 0 || tail < 0 || (unsigned)pick >= (unsigned)k.keep_rows;
-        if (seqs)
-            for (int t = lane; t < i; t += 64) bad |= s_seq[t] == s;
-        int len = 0;
-        if (!__any(bad)) {
-            len = kv_length(c, s);
-            bad = tail > len;
-        }
-        if (__any(bad)) {
-            if (lane == 0) {
-                s_end[i] = -1;
-                count[i] = 0;
-                if (status) status[i] = kRefused;
-            }
-            continue;
-        }
-        const int base = len - tail;
+// Judges the entries, a wave an entry: the moves are written down from the
+// table as it is, and the length to cut to.  Nothing is changed yet, so no
+// entry sees another's pages released.
+__global__ __launch_bounds__(kThreads) void kv_judge_kernel(KvCache c, const int32_t* seqs,
+                                                            KvKeep k, int n, int32_t* status,
+                                                            int32_t* ends, int32_t* count,
+                                                            Move* moves) {
+    const int lane = threadIdx.x & 63;
+    const int i = blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6);
+    if (i >= n) return;
+    const int s = kv_seq(c, seqs, i), tail = k.tails[i];
+    const int pick = k.pick ? k.pick[i] : 0;
+    bool bad = s < 0 || tail < 0 || (unsigned)pick >= (unsigned)k.keep_rows;
+    if (seqs)
+        for (int t = lane; t < i; t += 64) bad |= seqs[t] == s;
+    const int len = s < 0 ? 0 : kv_length(c, s);
+    bad |= tail > len;
+    bool refuse = __any(bad);
+    int kept = 0, n_moves = 0;
+    const int base = len - tail;
+    if (!refuse) {
         const int64_t row = (int64_t)i * k.keep_rows + pick;
         const int32_t* keep = k.keep + row * k.keep_ld;
         int most = k.keep_len[row];
         most = most < 0 ? 0 : (most < k.keep_ld ? most : k.keep_ld);
-        // The leading run of strictly ascending nodes of the tail.
-        int kept = most;
-        for (int j0 = 0; j0 < most; j0 += 64) {
+        // The leading run of strictly ascending nodes of the tail, and of them
+        // the rows that move; whether a page they go to is shared.
+        bool shared = false, more = true;
+        Move* out = moves + (int64_t)i * k.keep_ld;
+        for (int j0 = 0; j0 < most && more; j0 += 64) {
             const int j = j0 + lane;
             const int node = j < most ? keep[j] : 0;
             const int prev = j < most && j > 0 ? keep[j - 1] : -1;
-            const uint64_t stop = __ballot(j < most && (node <= prev || node >= tail));
-            if (stop) {
-                kept = j0 + __builtin_ctzll(stop);
-                break;
-            }
-        }
-        // Rows that move, and whether a page they go to is shared.
-        bool shared = false;
-        int n_moves = 0;
-        Move* out = moves + (int64_t)i * k.keep_ld;
-        for (int j0 = 0; j0 < kept; j0 += 64) {
-            const int j = j0 + lane;
-            bool go = j < kept && keep[j] != j;
+            const uint64_t stop = __ballot(j >= most || node <= prev || node >= tail);
+            const int wide = stop ? __builtin_ctzll(stop) : 64;
+            more = wide == 64;
+            kept += wide;
+            bool go = lane < wide && node != j;
             int64_t src = -1, dst = -1;
             if (go) {
-                src = cell_of(c, s, base + keep[j]);
+                src = cell_of(c, s, base + node);
                 dst = cell_of(c, s, base + j);
                 go = src >= 0 && dst >= 0;
                 if (go) shared |= c.page_refs[dst >> c.lg_page] > 1;
@@ -371,36 +354,39 @@ __global__ __launch_bounds__(kPlanThreads) void kv_compact_kernel(KvCache c, con
             }
             n_moves += __popcll(who);
         }
-        const bool refuse = __any(shared);
-        if (lane == 0) {
-            s_end[i] = refuse ? -1 : base + kept;
-            count[i] = refuse ? 0 : n_moves;
-            if (status) status[i] = refuse ? kRefused : kOk;
-        }
+        refuse = __any(shared);
     }
-    __syncthreads();
-    for (int i = wave; i < n; i += kPlanThreads / 64) {
-        const int end = s_end[i];
-        if (end < 0) continue;
-        const int s = s_seq[i];
-        const int len = kv_length(c, s);
-        release(c, s, pages_of(c, end), pages_of(c, len), lane, 64);
-        if (lane == 0) c.seq_len[s] = end;           // behind the wave's own read of it
+    if (lane == 0) {
+        ends[i] = refuse ? -1 : base + kept;
+        count[i] = refuse ? 0 : n_moves;
+        if (status) status[i] = refuse ? kRefused : kOk;
     }
 }
 
 // The moves of a (layer, K or V, head): a wave an entry's, in order.  A path's
 // nodes ascend, so a row goes to its own place or further to the front and
 // never onto a row that a later move reads; a wave's rows are all read before
-// the first of them is written.
+// the first of them is written.  The first waves cut the sequences instead:
+// the moves are in the list, so no other wave needs the table any more.
 template <int D>
-__global__ __launch_bounds__(kThreads) void kv_move_kernel(KvCache c, int n, int keep_ld,
+__global__ __launch_bounds__(kThreads) void kv_move_kernel(KvCache c, const int32_t* seqs, int n,
+                                                           int keep_ld, const int32_t* ends,
                                                            const int32_t* count,
                                                            const Move* moves) {
     constexpr int kPer = D / 32;                     // 16-byte parts of a row
     constexpr int kRows = 64 / kPer;                 // rows of a wave's step
     const int lane = threadIdx.x & 63;
-    const int64_t at = (int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6);
+    int64_t at = (int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6);
+    if (at < n) {
+        const int end = ends[at];
+        if (end < 0) return;
+        const int s = kv_seq(c, seqs, (int)at);
+        const int len = kv_length(c, s);
+        release(c, s, pages_of(c, end), pages_of(c, len), lane, 64);
+        if (lane == 0) c.seq_len[s] = end;
+        return;
+    }
+    at -= n;
     const int heads2 = 2 * c.heads;
     if (at >= (int64_t)n * c.n_layers * heads2) return;
     const int head = (int)(at % heads2);
@@ -475,28 +461,30 @@ hipError_t launch_kv_reserve(const KvCache& c, const int32_t* seqs, const int32_
 }
 
 size_t kv_compact_workspace_bytes(int n, int keep_ld) {
-    return align256((size_t)n * sizeof(int32_t)) + align256((size_t)n * keep_ld * sizeof(Move));
+    return align256((size_t)2 * n * sizeof(int32_t)) + align256((size_t)n * keep_ld * sizeof(Move));
 }
 
 hipError_t launch_kv_compact(const KvCache& c, const int32_t* seqs, const KvKeep& k, int n,
                              int32_t* status, void* workspace, hipStream_t st) {
-    int32_t* count = (int32_t*)workspace;
-    Move* moves = (Move*)((char*)workspace + align256((size_t)n * sizeof(int32_t)));
-    hipLaunchKernelGGL(kv_compact_kernel, dim3(1), dim3(kPlanThreads), 0, st, c, seqs, k, n,
-                       status, count, moves);
+    int32_t* ends = (int32_t*)workspace;
+    int32_t* count = ends + n;
+    Move* moves = (Move*)((char*)workspace + align256((size_t)2 * n * sizeof(int32_t)));
+    constexpr int kWaves = kThreads / 64;
+    hipLaunchKernelGGL(kv_judge_kernel, dim3((unsigned)((n + kWaves - 1) / kWaves)),
+                       dim3(kThreads), 0, st, c, seqs, k, n, status, ends, count, moves);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    const int64_t waves = (int64_t)n * c.n_layers * 2 * c.heads;
-    const dim3 grid((unsigned)((waves + kThreads / 64 - 1) / (kThreads / 64)));
+    const int64_t waves = n + (int64_t)n * c.n_layers * 2 * c.heads;
+    const dim3 grid((unsigned)((waves + kWaves - 1) / kWaves));
     if (c.d == 64)
-        hipLaunchKernelGGL((kv_move_kernel<64>), grid, dim3(kThreads), 0, st, c, n, k.keep_ld,
-                           count, moves);
+        hipLaunchKernelGGL((kv_move_kernel<64>), grid, dim3(kThreads), 0, st, c, seqs, n,
+                           k.keep_ld, ends, count, moves);
     else if (c.d == 128)
-        hipLaunchKernelGGL((kv_move_kernel<128>), grid, dim3(kThreads), 0, st, c, n, k.keep_ld,
-                           count, moves);
+        hipLaunchKernelGGL((kv_move_kernel<128>), grid, dim3(kThreads), 0, st, c, seqs, n,
+                           k.keep_ld, ends, count, moves);
     else
-        hipLaunchKernelGGL((kv_move_kernel<256>), grid, dim3(kThreads), 0, st, c, n, k.keep_ld,
-                           count, moves);
+        hipLaunchKernelGGL((kv_move_kernel<256>), grid, dim3(kThreads), 0, st, c, seqs, n,
+                           k.keep_ld, ends, count, moves);
     return hipGetLastError();
 }
 
