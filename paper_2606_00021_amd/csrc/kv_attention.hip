@@ -43,11 +43,12 @@ constexpr int kThreads = 256;
 constexpr int kWaves = 4;
 constexpr int kStep = 32;              // keys of a wave's step
 constexpr int kTile = kStep * kWaves;  // keys of a workgroup's step
-// A unit is not cut below this many keys: a shorter run costs more in joining
-// than its parallelism gains.
+// A unit is not cut into runs of fewer keys (one token over 2000 positions, 8
+// key heads: 10.4 us with 256, 11.5 with 512, 14.1 with 1024; 16 of them 17.9,
+// 16.8, 17.2), nor at all where no sequence is longer than kWhole, which saves
+// the second launch (500 positions 7.5 us whole, 10.0 cut; 1000 the same;
+// 2000 15.8 and 10.4).
 constexpr int kMinRun = 256;
-// Nor is any where no sequence is longer than this: a second launch takes
-// longer than the keys.
 constexpr int kWhole = 1024;
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
@@ -64,7 +65,6 @@ typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef const __attribute__((address_space(4))) int32_t* ScalarInts;
 
 constexpr int kTries = 3;              // run lengths tried
-constexpr int kXcdRun = 8;             // items of a run (tiles of more than 32 rows)
 
 struct Args {
     KvCache c;
@@ -122,19 +122,6 @@ __device__ __forceinline__ int64_t divide(int64_t a, int b) {
     return a >> 31 ? a / b : (int64_t)((unsigned)a / (unsigned)b);
 }
 
-// The item of this workgroup.  Workgroups are dealt to the 8 XCDs in turn;
-// items go to them in short runs, so that tiles which read the same keys share
-// an L2 and every XCD still has its part of each entry.
-template <int ROWS>
-__device__ __forceinline__ int item_of_block() {
-    constexpr int kRun = ROWS <= 32 ? 1 : kXcdRun;
-    const int idx = (int)(blockIdx.x >> 3);
-    // The run of an XCD moves on by one each time, or a period of the items'
-    // sizes could give one XCD all the large ones.
-    const int turn = idx / kRun;
-    return (turn * 8 + (int)((blockIdx.x + turn) & 7)) * kRun + idx % kRun;
-}
-
 // The items of up to 64 entries, in order, computed by every wave for itself
 // from the entries' lengths, a lane an entry.  The first workgroup leaves them
 // for the join.
@@ -167,7 +154,7 @@ __device__ __forceinline__ Plan plan_few(const Args& g) {
     if (g.target && blockIdx.x == 0 && threadIdx.x < g.b.n)
         g.plans[threadIdx.x] = i32x4{z0.rows, upto - mine, splits_of(z0.tiles, run), run};
     Plan p;
-    p.item = item_of_block<ROWS>();
+    p.item = (int)blockIdx.x;
     p.entry = -1;
     const uint64_t who = __ballot(p.item >= upto - mine && p.item < upto);
     if (!who) return p;
@@ -252,7 +239,7 @@ template <int ROWS>
 __device__ __forceinline__ Plan plan_many(const Args& g) {
     const int lane = threadIdx.x & 63;
     Plan p;
-    p.item = item_of_block<ROWS>();
+    p.item = (int)blockIdx.x;
     p.entry = -1;
     int from = 0, to = g.b.n + 1;               // the one behind the last holds the total
     while (to - from > 1) {
@@ -702,21 +689,6 @@ __global__ __launch_bounds__(kThreads, MT * D > 128 || MT == 2 ? 2 : (D == 128 ?
     }
 }
 
-// The tiles of a run of keys are items in this order: the last tiles first
-// (causal, they see the most keys), kXcdRun of a head side by side.
-__device__ __forceinline__ void tile_of(int at, int n_tiles, int heads, int* rt, int* head) {
-    const int block = at / (kXcdRun * heads), begin = block * kXcdRun;
-    const int wide = n_tiles - begin < kXcdRun ? n_tiles - begin : kXcdRun;
-    const int in = at - begin * heads;
-    *head = in / wide;
-    *rt = n_tiles - 1 - begin - in % wide;
-}
-__device__ __forceinline__ int place_of(int rt, int head, int n_tiles, int heads) {
-    const int back = n_tiles - 1 - rt, begin = back / kXcdRun * kXcdRun;
-    const int wide = n_tiles - begin < kXcdRun ? n_tiles - begin : kXcdRun;
-    return begin * heads + head * wide + back - begin;
-}
-
 // The same for many rows (draft trees, prompt chunks): a workgroup's four
 // waves have 16 MT rows each and share the keys.  A tile of KT keys is widened
 // once for all of them and laid into LDS in the order in which the matrix
@@ -745,8 +717,11 @@ __global__ __launch_bounds__(kThreads, D >= 128 ? 2 : 3) void kv_many_kernel(Arg
     const int n_tiles = (p.rows * g.group + kRows - 1) / kRows;
     const int local = p.item - p.first;
     const int split = local / (n_tiles * g.c.heads);
-    int rt, head;
-    tile_of(local % (n_tiles * g.c.heads), n_tiles, g.c.heads, &rt, &head);
+    // Tiles of one run from the last on (causal, they see the most keys), the
+    // heads of each side by side: workgroups are dealt to the 8 XCDs in turn,
+    // so the tiles of a head meet in one L2 where there are 8 heads.
+    const int at = local - split * n_tiles * g.c.heads;
+    const int rt = n_tiles - 1 - at / g.c.heads, head = at % g.c.heads;
     const int r0 = rt * kRows;
     const int w0 = r0 + wave * 16 * MT;         // the wave's rows
     const int base = p.len - p.rows;
@@ -1089,8 +1064,7 @@ __global__ __launch_bounds__(kThreads) void kv_join_kernel(Args g, int tiles_max
     if (splits == 1) return;
     const int n_tiles = (rows * g.group + ROWS - 1) / ROWS;
     if (rt >= n_tiles) return;
-    const int place =
-        ROWS <= 32 ? head * n_tiles + rt : place_of(rt, head, n_tiles, g.c.heads);
+    const int place = (n_tiles - 1 - rt) * g.c.heads + head;
     const int team = threadIdx.x / kLanes, dim = threadIdx.x % kLanes * 4;
     const int64_t start = kv_start(g.b, entry);
     for (int r = sub * RB + (RB == 1 ? 0 : team); r < (sub + 1) * RB; r += kTeams) {
@@ -1158,17 +1132,24 @@ __global__ __launch_bounds__(kThreads) void kv_join_kernel(Args g, int tiles_max
 }
 
 // Rows of a tile.  Up to 32 rows of a unit are one tile of the kernel whose
-// waves share rows; more go to the one whose waves share keys, in tiles of 128
-// (of 64 where the unit has no more, and of 256 dims, whose sums take twice
-// the registers).
+// waves share rows (24 rows of 128 dims over 3000 positions, 4 entries: 17.7
+// us, 18.5 by the other); more go to the one whose waves share keys, in tiles
+// of 128: two 2048-token chunks over 6000 positions 356 us, 497 in tiles of 64.
+// Tiles of 64 where the unit has no more, of 256 dims, whose sums take twice
+// the registers, and of 64 dims where they leave a quarter of the rows less
+// empty (183 rows, 16 entries over 2000 positions: 40.9 us, 44.2).
 int tile_rows(int max_rows, int group, int d) {
     const int64_t rows = (int64_t)max_rows * group;
     if (rows <= 16) return 16;
     if (rows <= 32 && d != 256) return 32;
-    return rows <= 64 || d == 256 ? 64 : 128;
+    if (rows <= 64 || d == 256) return 64;
+    const int64_t by64 = (rows + 63) / 64 * 64, by128 = (rows + 127) / 128 * 128;
+    return d == 64 && 4 * by64 <= 3 * by128 ? 64 : 128;
 }
 
-// Workgroups to cut the work for: what is resident at once.
+// Workgroups to cut the work for: what is resident at once (twice and three
+// times as many took 41 -> 46, 48 us for one token over 131K positions: each
+// costs its start and a partial sum).
 int target_items(int rows, int d) {
     if (rows > 32) return device_cus() * (d >= 128 ? 2 : 3);
     return device_cus() * (rows > 16 || d == 256 ? 2 : (d == 128 ? 3 : 4));
@@ -1187,9 +1168,7 @@ hipError_t launch_rows(const Args& g, hipStream_t st) {
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
-    // Whole runs for every XCD; at most target + units items.
-    const int64_t per = ROWS <= 32 ? 8 : 8 * kXcdRun;
-    const dim3 grid((unsigned)((units + g.target + per - 1) / per * per));
+    const dim3 grid((unsigned)(units + g.target));      // items, at most
     if constexpr (ROWS <= 32)
         hipLaunchKernelGGL((kv_few_kernel<D, F16, ROWS / 16>), grid, dim3(kThreads), 0, st, g);
     else
@@ -1221,7 +1200,7 @@ int64_t kv_attention_blocks(int n, int max_rows, int n_heads, int kv_heads, int 
     const int rows = tile_rows(max_rows, n_heads / kv_heads, d);
     const int64_t units = units_most(n, max_rows, n_heads, kv_heads, rows);
     // Of the attention itself, and of the join (a workgroup for 1 or 16 rows).
-    return units * (rows == 16 ? 16 : rows / 16) + target_items(rows, d) + 8 * kXcdRun;
+    return units * (rows == 16 ? 16 : rows / 16) + target_items(rows, d);
 }
 
 // Partial sums, where units may be cut, and the entries' plans.

@@ -232,6 +232,30 @@ def test_many_entries():
     for i, n in enumerate(lens):
         if n == 0:
             assert (out[i] == 0).all()
+    # whole units (a bound that cuts none), and sequences in another order
+    assert torch.equal(sense.sense_kv_attention(kvc, 0, q, max_kv=900)[5], out[5])
+    order = rng.permutation(333)
+    perm = torch.tensor(order, device=DEV)
+    whole = sense.sense_kv_attention(kvc, 0, q[perm], seqs=ints(order), max_kv=900)
+    for i in (0, 64, 332, int(np.nonzero(order == 100)[0][0])):
+        compare(whole[i:i + 1], q[order[i]:order[i] + 1], m, 0, [int(order[i])], [1])
+
+
+def test_many_chunks():
+    """More than 64 entries of many rows each, some without any."""
+    print("[kv attention] many chunks", flush=True)
+    rng = np.random.default_rng(14)
+    counts = rng.integers(0, 50, 70).tolist()
+    counts[3], counts[69] = 0, 50
+    lens = [c + int(e) for c, e in zip(counts, rng.integers(0, 200, 70))]
+    lens[20] += 1500
+    kvc, m = pair(rng, lens, page=32, heads=2, d=64)
+    q = queries(rng, (70, 50, 6, 64), "f16")
+    out = torch.full_like(q, 3)
+    sense.sense_kv_attention(kvc, 0, q, row_len=ints(counts), out=out)
+    for i in (0, 3, 20, 63, 64, 65, 69):
+        compare(out[i:i + 1], q[i:i + 1], m, 0, [i], [counts[i]])
+        assert (out[i, counts[i]:] == 3).all()
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
