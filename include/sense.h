@@ -686,7 +686,8 @@ typedef struct {
  * (max_rows when NULL; clamped to [0, max_rows]): row j of the entry is row
  * row_start[i] + j of the tensors (i * max_rows + j when NULL) and stands for
  * position seq_len - m + j, the last m positions of the sequence.  Rows outside
- * [0, n_rows), positions below 0 and entries of no sequence are left out.
+ * [0, n_rows), positions below 0 and entries of no sequence are left out; a
+ * row of an output that belongs to two entries is written by either.
  * n <= 65536, 1 <= max_rows <= 2^20; arrays are DEVICE memory. */
 typedef struct {
     const int32_t *seqs;
@@ -750,8 +751,10 @@ sense_status_t sense_kv_attention_workspace_size(const sense_kv_cache_t *cache, 
  * (for a draft tree the mask of sense_build_loose_trie, row_len its tree_len).
  * A row that sees nothing becomes 0.  Positions that a row does not see do not
  * touch it, whatever they hold.  Statistics and sums are fp32; cached values
- * enter in q_dtype (exact in BF16; in F16 within its range), weights are
- * rounded to q_dtype.
+ * enter in q_dtype (exact in BF16 for all that sense_kv_write writes; F16 has
+ * to hold them: a row that sees a block of a scale above 2^13 is unspecified),
+ * weights are rounded to q_dtype.  NaN that a row sees makes it NaN: a key's
+ * the whole row, a value's the dims of its block.
  *   q, out      rows of n_heads x head_dim elements of q_dtype (F16, BF16),
  *               head h at h * head_dim; strides in elements; bases and strides
  *               multiples of 16 bytes.  out may be q.  Rows that the batch

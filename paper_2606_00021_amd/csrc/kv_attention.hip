@@ -7,13 +7,21 @@
 // exp(s - m) and exp(s - m) v are kept in fp32, rescaled only when a weight
 // passes 2^8.
 //
-// A unit is the rows of one entry that share a key head: new tokens times
-// query heads per key head, in tiles of 16 MT rows.  A unit's keys are cut
-// into runs of C keys; an item is one tile over one run, and a workgroup has
-// one item, its four waves taking steps of 32 keys in turn.  C is computed on
-// the device from the lengths themselves (plan()), so that about `target`
-// workgroups share the work whatever the lengths are; runs of one unit are
-// joined by a second kernel.
+// The rows of one entry that share a key head (new tokens times query heads
+// per key head) are cut into tiles; a unit is one tile.  A unit's keys are cut
+// into runs, an item is a unit over one run, and a workgroup has one item.
+// The length of a run is computed on the device from the sequences' lengths
+// (plan()), so that about `target` workgroups share the work whatever the
+// lengths are; a second kernel joins the runs of a unit.  Up to 32 rows the
+// four waves of a workgroup have the same rows and take steps of 32 keys in
+// turn (kv_few_kernel), beyond they have rows of their own and share the keys
+// (kv_many_kernel).
+//
+// Few rows are bound by the bytes of the cache: 64 streams of 8000 positions
+// (32 / 8 heads of 128, 557 MB) take 109 us, 5.1 TB/s, where a plain read of as
+// many bytes takes 80.  Many rows are bound by the matrix and vector units
+// (exponentials): two 2048-token chunks over 6000 positions 356 us, 937
+// TFLOP/s, where a large bf16 product of the library reaches 1170.
 //
 // Both products run on the matrix cores, transposed:
 //   S^T = K Q^T   A = K (16 keys x 32 dims), B = Q^T (32 dims x 16 rows)
@@ -26,13 +34,13 @@
 //   - in the second product lane (m, g) has keys 4g .. 4g+3 of both key tiles
 //     and dims [m d/16, (m+1) d/16): whole bytes of codes, of one scale a key.
 //     Codes of two keys are widened by v_cvt_scalef32_pk and exchanged in
-//     pairs by v_perm, so nothing passes through LDS.
+//     pairs by v_perm.
 // A key tile lies in one page, so every load has a base that is the same for
 // the wave and an offset that is the same for all steps.
 // 4-bit values times their scales are exact in bf16, and in f16 where they lie
-// in its range.  Probabilities are rounded to the query's type (nearest);
-// their sum is taken of the rounded ones, by a product with ones, so that the
-// weights that are used add up to 1.
+// in its range.  Weights are rounded to the query's type (nearest), which is
+// off by as much as rounding the result is; their sum is taken of the rounded
+// ones, by a product with ones, so that the weights that are used add up to 1.
 #include "internal.h"
 #include "kv.h"
 
@@ -317,6 +325,12 @@ __device__ __forceinline__ bool row_over(uint32_t most, uint32_t limit) {
 __device__ __forceinline__ float unit_of(uint32_t byte) {
     return __builtin_bit_cast(float, byte << 23);
 }
+// The largest unit whose codes are all finite in the type.  A weight of 0 must
+// meet a finite value, whatever lies in a position that a row does not see.
+template <bool F16>
+__device__ __forceinline__ float finite_unit(float unit) {
+    return fminf(unit, F16 ? 0x1p13f : 0x1p125f);
+}
 
 // Which of 4 N positions a row sees: bit 4t + r is position first + 16t + r,
 // with `none` the tiles that have no page (bit `stride` t).  The mask's bytes
@@ -365,7 +379,8 @@ struct Pages {
 };
 
 template <int D, bool F16, int MT>
-__global__ __launch_bounds__(kThreads, MT * D > 128 || MT == 2 ? 2 : (D == 128 ? 3 : 4)) void kv_few_kernel(Args g) {
+__global__ __launch_bounds__(kThreads, MT * D > 128 || MT == 2 ? 2 : (D == 128 ? 3 : 4))
+    void kv_few_kernel(Args g) {
     constexpr int kRows = 16 * MT;
     constexpr int kKs = D / 32;         // matrix steps of the first product
     constexpr int DV = D / 16;          // dims of a lane in the second
@@ -578,7 +593,7 @@ __global__ __launch_bounds__(kThreads, MT * D > 128 || MT == 2 ? 2 : (D == 128 ?
                 const bool here = __builtin_bit_cast(uint32_t, unit[i]) == 0x7F800000u;
                 some |= here;
                 nan[i >> 1] |= here ? (i & 1 ? one & 0xFFFF0000u : one & 0xFFFFu) : 0u;
-                unit[i] = here ? 0.f : unit[i];
+                unit[i] = here ? 0.f : finite_unit<F16>(unit[i]);
             }
             if (__any(some)) {
 #pragma unroll
@@ -838,7 +853,7 @@ __global__ __launch_bounds__(kThreads, D >= 128 ? 2 : 3) void kv_many_kernel(Arg
                 const bool here = byte == 255u;
                 some |= here;
                 nan[i >> 1] |= here ? (i & 1 ? one & 0xFFFF0000u : one & 0xFFFFu) : 0u;
-                unit[i] = here ? 0.f : unit_of(byte);
+                unit[i] = here ? 0.f : finite_unit<F16>(unit_of(byte));
             }
             const int step = part >> 1, half = part & 1;
             const bool any = __any(some);

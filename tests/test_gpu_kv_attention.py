@@ -297,6 +297,37 @@ def test_what_a_row_does_not_see_does_not_touch_it(dtype, d):
         assert torch.equal(got[i].cpu()[~want], clean[i].cpu()[~want])
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("d,nodes", [(64, 3), (128, 40), (256, 9)])
+def test_unseen_positions_may_hold_anything(dtype, d, nodes):
+    """Any byte as a code or scale behind the end and in free pages, and tree
+    nodes of the largest scales that most rows do not see."""
+    print(f"[kv attention] unseen bytes {dtype} d={d} nodes={nodes}", flush=True)
+    rng = np.random.default_rng(d + nodes)
+    lens = [nodes, 301, 77 + nodes]
+    kvc, m = pair(rng, lens, page=32, heads=1, d=d)
+    masks = np.repeat(np.eye(nodes, dtype=np.uint8)[None], 3, 0)
+    masks[:, -1, 0] = 1
+    gmask = torch.tensor(masks, device=DEV)
+    q = queries(rng, (3, nodes, 4, d), dtype)
+    clean = sense.sense_kv_attention(kvc, 0, q, mask=gmask)
+    dirty = {k: v.clone() for k, v in kvc.items()}
+    free = torch.ones(m.refs.size, dtype=torch.bool, device=DEV)
+    for s, n in enumerate(lens):
+        free[torch.tensor(m.table[s][m.table[s] >= 0], device=DEV).long()] = False
+        if n % 32:
+            tail = dirty["scales"][:, int(m.table[s, n // 32]), :, :, :, n % 32:]
+            tail.copy_(torch.randint(0, 256, tail.shape, device=DEV))
+        pg, slot = m.cell(s, n - nodes + 1)
+        dirty["scales"][0, int(pg), :, :, :, int(slot)] = 254
+        dirty["codes"][0, int(pg), :, :, int(slot)] = 0xF7
+    dirty["scales"][:, free] = 254
+    dirty["codes"][:, free] = 0x77
+    got = sense.sense_kv_attention(dirty, 0, q, mask=gmask)
+    rows = [u for u in range(nodes) if u != 1]                 # node 1 sees itself
+    assert torch.equal(got[:, rows], clean[:, rows])
+
+
 def test_seen_nan_in_the_prefix_reaches_every_row():
     print("[kv attention] seen NaN", flush=True)
     rng = np.random.default_rng(6)
