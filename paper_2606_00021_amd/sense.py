@@ -990,15 +990,20 @@ def _kv_on(cache: dict, stream, call):
 
 
 def _kv_scratch(cache: dict, workspace: torch.Tensor | None, size_call: str, *args):
-    """The caller's workspace, or one of the size that ``size_call`` names."""
+    """The caller's workspace, or one of the size that ``size_call`` names
+    (None where that is 0)."""
     if workspace is None:
         size = ctypes.c_size_t()
         _check(getattr(load_library(), size_call)(*args, ctypes.byref(size)), size_call)
-        return cache["codes"].new_empty(max(size.value, 1))
+        return cache["codes"].new_empty(size.value) if size.value else None
     if workspace.dtype != torch.uint8 or not workspace.is_contiguous() \
             or workspace.device != cache["codes"].device:
         raise ValueError("workspace must be a contiguous uint8 tensor on the cache's device")
     return workspace
+
+
+def _kv_span(workspace: torch.Tensor | None):
+    return (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel())
 
 
 def _kv_ints(t: torch.Tensor | None, n: int | None, cache: dict, name: str):
@@ -1152,7 +1157,7 @@ def sense_kv_attention(cache: dict, layer: int, q: torch.Tensor, mask: torch.Ten
             _kv_row_stride(q, 0, "q"), ctypes.byref(batch),
             None if mask is None else mask.data_ptr(), ld, step,
             q.shape[-1] ** -0.5 if softmax_scale is None else softmax_scale, max_kv,
-            o.data_ptr(), _kv_row_stride(o, 0, "out"), ws.data_ptr(), ws.numel(), st),
+            o.data_ptr(), _kv_row_stride(o, 0, "out"), *_kv_span(ws), st),
             "sense_kv_attention")
         return o
 
@@ -1210,7 +1215,7 @@ def sense_kv_reserve(cache: dict, counts: torch.Tensor, seqs: torch.Tensor | Non
         _check(load_library().sense_kv_reserve(
             ctypes.byref(desc), _kv_ints(seqs, n, cache, "seqs"),
             _kv_ints(counts, n, cache, "counts"), n, status.data_ptr(),
-            ws.data_ptr(), ws.numel(), st), "sense_kv_reserve")
+            *_kv_span(ws), st), "sense_kv_reserve")
         return status
 
     return _kv_on(cache, stream, call)
@@ -1242,7 +1247,7 @@ def sense_kv_compact(cache: dict, tails: torch.Tensor, keep: torch.Tensor,
             _kv_ints(tails, n, cache, "tails"), _kv_ints(keep, None, cache, "keep"),
             _kv_ints(keep_len, n * rows, cache, "keep_len"), _kv_ints(pick, n, cache, "pick"),
             max(rows, 1), keep.shape[-1], n, status.data_ptr(),
-            ws.data_ptr(), ws.numel(), st), "sense_kv_compact")
+            *_kv_span(ws), st), "sense_kv_compact")
         return status
 
     return _kv_on(cache, stream, call)
