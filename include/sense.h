@@ -761,7 +761,7 @@ sense_status_t sense_kv_attention_workspace_size(const sense_kv_cache_t *cache, 
  *               leaves out keep their contents.
  *   n_heads     a multiple of n_kv_heads, at most 4096.
  *   mask        uint8 (DEVICE) or NULL; mask_ld >= max_rows.
- *   softmax_scale  positive and finite.
+ *   softmax_scale  in (0, 2^127].
  *   max_kv      a bound on the lengths (0: the capacity).  Longer sequences
  *               are attended in full all the same; the bound sizes the
  *               workspace, and where it is small the call is one launch.

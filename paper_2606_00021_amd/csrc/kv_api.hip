@@ -235,8 +235,8 @@ SENSE_EXPORT sense_status_t sense_kv_attention(
         return fail(SENSE_ERR_INVALID_ARGUMENT, "q_dtype = %d is neither F16 nor BF16",
                     (int)q_dtype);
     if ((s = check_heads(n_heads, c.heads)) != SENSE_OK) return s;
-    if (!(softmax_scale > 0.f) || !(softmax_scale < INFINITY))
-        return fail(SENSE_ERR_INVALID_ARGUMENT, "softmax_scale = %g is not positive and finite",
+    if (!(softmax_scale > 0.f) || !(softmax_scale <= 0x1p127f))
+        return fail(SENSE_ERR_INVALID_ARGUMENT, "softmax_scale = %g outside (0, 2^127]",
                     (double)softmax_scale);
     if (max_kv < 0) return fail(SENSE_ERR_INVALID_ARGUMENT, "max_kv = %d < 0", max_kv);
     if (mask && (mask_ld < b.max_rows || mask_stride < 0))

@@ -81,7 +81,7 @@ struct Args {
     int group;          // query heads per key head
     int target;         // workgroups that the work is cut for (0: units stay whole)
     float* part_o;      // [item][rows][d]
-    f32x2* part_ml;     // [item][rows]: reference, sum
+    f32x2* part_ml;     // [item][rows]: reference (a score), sum
     i32x4* plans;       // [entry]: new tokens, first item, runs of a unit, tiles of a run
 };
 
@@ -322,6 +322,29 @@ __device__ __forceinline__ bool row_over(uint32_t most, uint32_t limit) {
     return (over | over >> 16 | over >> 32 | over >> 48) >> (threadIdx.x & 15) & 1;
 }
 
+// Weights of a row with the reference `now` (a score): 2^(cs (s - now) + lift),
+// computed as fma(s - sub, cs, add).  The step's one fma (sub 0, add = neg) is
+// off by a factor 2^r, r the rounding of cs now, which cancels in the row but
+// leaves the types of weights from cs now = 2^28 on.  Such rows, and those that
+// have seen nothing, have neg infinite, so that each step comes back here.
+struct Exponent {
+    float sub, add, neg;
+};
+__device__ __forceinline__ Exponent exponent(float now, float cs, float lift) {
+    const float at = now * cs;
+    const bool none = now == -INFINITY, far = !none && fabsf(at) >= 0x1p24f;
+    Exponent x;
+    x.sub = far ? now : 0.f;
+    x.add = none || far ? lift : lift - at;
+    x.neg = none || far ? INFINITY : x.add;
+    return x;
+}
+// What sums of reference `was` are worth at the reference `now`.  A row that
+// has seen nothing has sums of 0 (or of NaN scores).
+__device__ __forceinline__ float fade(float was, float now, float cs) {
+    return was == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((was - now) * cs);
+}
+
 __device__ __forceinline__ float unit_of(uint32_t byte) {
     return __builtin_bit_cast(float, byte << 23);
 }
@@ -433,7 +456,7 @@ __global__ __launch_bounds__(kThreads, MT * D > 128 || MT == 2 ? 2 : (D == 128 ?
     f32x4 o[DV][MT];
     f32x4 lsum[MT];
     f32x4 hit[MT];                      // NaN values that a row sees, for its dims
-    float ref[MT], neg[MT];             // reference of the exponents; kLift - it, or infinity
+    float ref[MT], neg[MT];             // reference of the weights, see exponent()
     constexpr float kLift = F16 ? 7.f : 0.f;    // f16: weights up to 2^15, not 2^8
     constexpr uint32_t kMostBits = (uint32_t)(127 + (F16 ? 15 : 8)) << 23;
 #pragma unroll
@@ -554,17 +577,17 @@ __global__ __launch_bounds__(kThreads, MT * D > 128 || MT == 2 ? 2 : (D == 128 ?
                 float now = s[mt][0][0];
 #pragma unroll
                 for (int i = 1; i < 8; ++i) now = fmaxf(now, s[mt][i >> 2][i & 3]);
-                now *= cs;
                 now = fmaxf(now, __shfl_xor(now, 16));
                 now = fmaxf(fmaxf(now, __shfl_xor(now, 32)), ref[mt]);
                 now = row_over(most[mt], kMostBits) ? now : ref[mt];
-                const float keep = now == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ref[mt] - now);
-                const float use = now == -INFINITY ? kLift : kLift - now;
+                const float keep = fade(ref[mt], now, cs);
+                const Exponent x = exponent(now, cs, kLift);
                 ref[mt] = now;
-                neg[mt] = now == -INFINITY ? INFINITY : use;
+                neg[mt] = x.neg;
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
-                    w[mt][i] = __builtin_amdgcn_exp2f(fmaf(s[mt][i >> 2][i & 3], cs, use));
+                    w[mt][i] =
+                        __builtin_amdgcn_exp2f(fmaf(s[mt][i >> 2][i & 3] - x.sub, cs, x.add));
 #pragma unroll
                 for (int t = 0; t < DV; ++t) o[t][mt] *= keep;
                 lsum[mt] *= keep;
@@ -684,9 +707,7 @@ __global__ __launch_bounds__(kThreads, MT * D > 128 || MT == 2 ? 2 : (D == 128 ?
         f32x4 sum = {0, 0, 0, 0};
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) {
-            // A wave that saw no key has sums of 0 (or of NaN scores).
-            const float f =
-                s_m[w][r] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(s_m[w][r] - top);
+            const float f = fade(s_m[w][r], top, cs);
             l += s_l[w][r] * f;
             sum += *(const f32x4*)&s_o[w][r][dim] * f;
         }
@@ -938,18 +959,17 @@ __global__ __launch_bounds__(kThreads, D >= 128 ? 2 : 3) void kv_many_kernel(Arg
                 float now = s[mt][0][0];
 #pragma unroll
                 for (int i = 1; i < 4 * kTiles; ++i) now = fmaxf(now, s[mt][i >> 2][i & 3]);
-                now *= cs;
                 now = fmaxf(now, __shfl_xor(now, 16));
                 now = fmaxf(fmaxf(now, __shfl_xor(now, 32)), ref[mt]);
                 now = row_over(most[mt], kMostBits) ? now : ref[mt];
-                const float keep = now == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ref[mt] - now);
-                const float use = now == -INFINITY ? kLift : kLift - now;
+                const float keep = fade(ref[mt], now, cs);
+                const Exponent x = exponent(now, cs, kLift);
                 ref[mt] = now;
-                neg[mt] = now == -INFINITY ? INFINITY : use;
+                neg[mt] = x.neg;
 #pragma unroll
                 for (int i = 0; i < 4 * kTiles; ++i)
                     s[mt][i >> 2][i & 3] =
-                        __builtin_amdgcn_exp2f(fmaf(s[mt][i >> 2][i & 3], cs, use));
+                        __builtin_amdgcn_exp2f(fmaf(s[mt][i >> 2][i & 3] - x.sub, cs, x.add));
 #pragma unroll
                 for (int t = 0; t < DV; ++t) o[t][mt] *= keep;
                 lsum[mt] *= keep;
@@ -1082,6 +1102,7 @@ __global__ __launch_bounds__(kThreads) void kv_join_kernel(Args g, int tiles_max
     const int place = (n_tiles - 1 - rt) * g.c.heads + head;
     const int team = threadIdx.x / kLanes, dim = threadIdx.x % kLanes * 4;
     const int64_t start = kv_start(g.b, entry);
+    const float cs = g.a.scale * 1.4426950408889634f;
     for (int r = sub * RB + (RB == 1 ? 0 : team); r < (sub + 1) * RB; r += kTeams) {
         const int rr = rt * ROWS + r, token = rr / g.group;
         const int64_t row = start + token;
@@ -1108,12 +1129,12 @@ __global__ __launch_bounds__(kThreads) void kv_join_kernel(Args g, int tiles_max
                 float now = top;
 #pragma unroll
                 for (int i = 0; i < kBatch; ++i) now = fmaxf(now, ml[i][0]);
-                const float a = top == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(top - now);
+                const float a = fade(top, now, cs);
                 l *= a;
                 sum *= a;
 #pragma unroll
                 for (int i = 0; i < kBatch; ++i) {
-                    float w = ml[i][0] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ml[i][0] - now);
+                    float w = fade(ml[i][0], now, cs);
                     w = s0 + i * kEvery < splits ? w : 0.f;
                     l += ml[i][1] * w;
                     sum += x[i] * w;
@@ -1128,9 +1149,7 @@ __global__ __launch_bounds__(kThreads) void kv_join_kernel(Args g, int tiles_max
             if (team != 0) return;
             for (int t = 1; t < kTeams; ++t) {
                 const float now = fmaxf(top, s_ml[t][0]);
-                const float a = top == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(top - now);
-                const float b =
-                    s_ml[t][0] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(s_ml[t][0] - now);
+                const float a = fade(top, now, cs), b = fade(s_ml[t][0], now, cs);
                 l = l * a + s_ml[t][1] * b;
                 sum = sum * a + s_o[t][threadIdx.x % kLanes] * b;
                 top = now;

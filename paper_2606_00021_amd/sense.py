@@ -1124,7 +1124,7 @@ def sense_kv_attention(cache: dict, layer: int, q: torch.Tensor, mask: torch.Ten
     [n, nodes, nodes], nodes >= max_rows: sense_build_loose_trie's) all
     positions in front of the entry's rows and those rows u that
     mask[i, j, u] names.  ``max_kv`` bounds the sequences' lengths (0: the
-    capacity); ``softmax_scale`` is d**-0.5 by default.  Returns ``out``
+    capacity); ``softmax_scale`` (in (0, 2^127]) is d**-0.5 by default.  Returns ``out``
     (like q; rows that belong to no entry keep what they hold)."""
     desc = _kv_desc(cache)
     dev = cache["codes"].device

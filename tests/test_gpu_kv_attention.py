@@ -1,7 +1,7 @@
 """Attention over the 4-bit cache against the definition in 64 bits.
 
-Bound of one output value, with u the half step of q's type (bf16 2^-8 / 2,
-as finfo.eps / 2), o the exact value and spread = sum w |v - o| / sum w:
+Bound of one output value, with u the half step of q's type (bf16 2^-8,
+f16 2^-11), o the exact value and spread = sum w |v - o| / sum w:
   u |o|                 the output's own rounding
   u spread              every weight is rounded once, and normalised by the sum
                         of the rounded ones
@@ -428,3 +428,39 @@ def test_other_streams_and_replays():
         grown = ints([40 * (turn + 1), 3])
         sense.sense_kv_reserve(kvc, grown)
         m.reserve([0, 1], grown.tolist())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("rows,heads", [(1, 2), (9, 3), (40, 4)])
+def test_scores_beyond_what_their_differences_resolve(dtype, d, rows, heads):
+    """Scores that are exact in fp32 and differ by far more than weights reach
+    (or not at all), up to 2^144: a row is the mean of its best positions'
+    values.  Bound: weights are 0 or equal, so the output's rounding and the
+    sums' alone."""
+    print(f"[kv attention] huge scores {dtype} d={d} rows={rows}", flush=True)
+    rng = np.random.default_rng(d + rows)
+    lens = [2500, 700, 300]
+    kvc, m = pair(rng, lens, page=32, heads=1, d=d)
+    # A key is its code's value in dim 5 and 0 elsewhere; scales as they are.
+    m.codes[:, :, 0] = 0
+    m.codes[:, :, 0, :, :, 2] = rng.integers(0, 16, m.codes[:, :, 0, :, :, 2].shape) << 4
+    kvc = up(m)
+    gains = torch.tensor([2.0 ** 14, -(2.0 ** 13), 3.0, 0.0])[:heads]
+    q = torch.zeros((3, rows, heads, d), dtype=DT[dtype], device=DEV)
+    q[..., 5] = gains.to(DEV)
+    u = torch.finfo(q.dtype).eps / 2
+    held = [m.rows(0, i, 0, n)[:, :, 0] for i, n in enumerate(lens)]
+    for scale in (2.0 ** 12, 3.0 * 2.0 ** 15, 2.0 ** 127):
+        out = sense.sense_kv_attention(kvc, 0, q, softmax_scale=scale).double().cpu()
+        for i, n in enumerate(lens):
+            k, v = held[i]
+            for h in range(heads):
+                s = k[:, 5] * float(gains[h])
+                for j in range(rows):
+                    end = n - rows + j + 1
+                    best = s[:end] == s[:end].max()
+                    ref = torch.tensor(v[:end][best].mean(0))
+                    tol = u * ref.abs() + 2.0 ** -25 + (n + 8) * 2.0 ** -23 * np.abs(v).max()
+                    off = (out[i, j, h] - ref).abs()
+                    assert (off <= tol).all(), (scale, i, h, j, float((off / tol).max()))

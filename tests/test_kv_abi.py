@@ -101,7 +101,7 @@ def test_bad_rows(lib, kw, status):
     (dict(layer=2), INVALID), (dict(dtype=0), INVALID), (dict(dtype=9), INVALID),
     (dict(heads=3), INVALID), (dict(heads=0), INVALID), (dict(heads=4098), INVALID),
     (dict(scale=0.0), INVALID), (dict(scale=-1.0), INVALID), (dict(scale=float("nan")), INVALID),
-    (dict(scale=float("inf")), INVALID), (dict(max_kv=-1), INVALID),
+    (dict(scale=float("inf")), INVALID), (dict(scale=2.0 ** 127 * 1.25), INVALID), (dict(max_kv=-1), INVALID),
     (dict(mask=FAKE, mask_ld=3), INVALID), (dict(mask=FAKE, mask_ld=4, mask_stride=-1), INVALID),
     (dict(q=None), INVALID), (dict(out=None), INVALID), (dict(q_stride=255), INVALID),
     (dict(q_stride=257), MISALIGNED), (dict(q=FAKE + 4), MISALIGNED), (dict(out=FAKE + 8), MISALIGNED),
