@@ -8,7 +8,10 @@
 // move is small (tables, one page a sequence, a path of some tokens a layer),
 // so these kernels are bound by launches and by the latency of dependent
 // loads: one launch that decides (a single workgroup where entries depend on
-// each other), then one over all layers for the bytes.
+// each other), then one over all layers for the bytes.  32 streams' 64-node
+// trees: room 7.0 us and 2.2 for no copy, path judged in 4.0 and moved in 3.8
+// (8 layers of 8 heads); 64 forks that each copy a page in every layer: 46.8
+// us, 5.4 TB/s.
 #include "internal.h"
 #include "kv.h"
 

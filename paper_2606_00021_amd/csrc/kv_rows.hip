@@ -9,10 +9,13 @@
 // Both move every byte once (2.53 bytes a 16-bit value) and do a few
 // operations on it.  A thread has 8 values: 16 bytes of a 16-bit row, 4 bytes
 // of codes; the four threads of a block find its largest value with two lane
-// exchanges.  A workgroup takes up to 16 tokens (of 128 values) of one head
-// side by side, so that the codes of a page's head leave as one run and a
-// block's scales as neighbouring bytes; a call of few tokens fills the
-// workgroup with more heads instead.
+// exchanges.  A workgroup takes up to 16 tokens (of 128 values) side by side,
+// so that the codes of a page's head leave as one run and a block's scales as
+// neighbouring bytes, of one head after the other where there is work for the
+// whole device; a call of few tokens puts heads beside each other instead.
+// 8 x 2048 rows of 8 heads of 128, keys and values, 85 MB: written in 17.0 us
+// (5.0 TB/s), read back in 18.1 (4.7), a large copy reaches 4.9; 61 rows 3.3
+// and 3.0 us.
 #include "internal.h"
 #include "kv.h"
 
@@ -68,11 +71,11 @@ __device__ __forceinline__ void store8(void* p, int64_t at, const float* x) {
 // A thread's token: which row of the tensors, and where in the cache.
 struct Place {
     int64_t row;     // row of the tensors
-    int64_t page;    // page * rows of a page's K (or V, or head 0) ...
+    int64_t page;    // its number; slot: the token's place in it
     int slot;
     int seq;
     bool ok;         // the token exists
-    bool page_ok;
+    bool page_ok;    // and has a page
 };
 
 // How a launch is cut: a workgroup has 2^lg tokens of one entry side by side

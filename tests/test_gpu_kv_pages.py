@@ -189,3 +189,35 @@ def test_tables_that_make_no_sense_stay_in_bounds():
     m.truncate([0], [10])
     assert kv["seq_len"][0].item() == 10 and kv["seq_len"][1].item() == 10
     assert np.array_equal(kv["page_table"][0].cpu().numpy(), m.table[0])
+
+
+def test_offsets_beyond_32_bits():
+    """A copy and a path at the end of a cache of more than 4 GiB."""
+    print("[kv pages] large", flush=True)
+    layers, pages, page, heads, d, n = 9, 4096, 128, 8, 128, 100
+    old, new = pages - 1, pages - 2
+    kv = {"codes": torch.zeros((layers, pages, 2, heads, page, d // 2), dtype=torch.uint8, device=DEV),
+          "scales": torch.zeros((layers, pages, 2, heads, d // 32, page), dtype=torch.uint8, device=DEV),
+          "page_table": ints([[old], [-1]]), "seq_len": ints([n, 0]),
+          "page_refs": torch.ones(pages, dtype=torch.int32, device=DEV)}
+    assert kv["codes"].numel() > 1 << 32
+    kv["page_refs"][new] = 0                                  # the one free page
+    for name, hi in (("codes", 256), ("scales", 255)):
+        t = kv[name][:, old]
+        t.copy_(torch.randint(0, hi, t.shape, dtype=torch.uint8, device=DEV))
+    codes, scales = kv["codes"][:, old].clone(), kv["scales"][:, old].clone()
+    assert sense.sense_kv_fork(kv, ints([0]), ints([1])).tolist() == [0]
+    assert sense.sense_kv_reserve(kv, ints([1]), ints([1])).tolist() == [0]
+    assert kv["page_table"].tolist() == [[old], [new]] and kv["seq_len"].tolist() == [n, n + 1]
+    assert kv["page_refs"][[old, new]].tolist() == [1, 1]
+    assert torch.equal(kv["codes"][:, new, :, :, :n], codes[:, :, :, :n])
+    assert torch.equal(kv["scales"][:, new, :, :, :, :n], scales[..., :n])
+    keep = [0, 3, 4, 18]
+    assert sense.sense_kv_compact(kv, ints([20]), ints([keep]), ints([4]), seqs=ints([1])).tolist() == [0]
+    base = n + 1 - 20
+    at = list(range(base)) + [base + u for u in keep]
+    assert kv["seq_len"].tolist() == [n, base + 4]
+    assert torch.equal(kv["codes"][:, new, :, :, :base + 4], codes[:, :, :, at])
+    assert torch.equal(kv["scales"][:, new, :, :, :, :base + 4], scales[..., at])
+    assert torch.equal(kv["codes"][:, old], codes) and torch.equal(kv["scales"][:, old], scales)
+    assert int(kv["codes"][:, :new].count_nonzero()) == int(kv["scales"][:, :new].count_nonzero()) == 0
