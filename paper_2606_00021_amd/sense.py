@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from dataclasses import dataclass
 
 import torch
@@ -186,6 +187,9 @@ class KvCacheDesc(ctypes.Structure):
         ("n_seqs", ctypes.c_int32),
         ("max_pages", ctypes.c_int32),
     ]
+
+
+_KV_CACHE_FIELDS = struct.Struct("@5P7i4x")      # KvCacheDesc
 
 
 class KvBatchDesc(ctypes.Structure):
@@ -949,6 +953,8 @@ def sense_build_kv_cache(n_layers: int, n_pages: int, page_size: int, n_kv_heads
 
 
 def _kv_desc(cache: dict) -> KvCacheDesc:
+    # Device numbers and one packing: compared and set one by one these checks
+    # are the largest part of a small call's host work (2.3 us, so 1.5).
     codes, scales = cache["codes"], cache["scales"]
     table, lens, refs = cache["page_table"], cache["seq_len"], cache["page_refs"]
     if codes.dim() != 6 or table.dim() != 2:
@@ -960,24 +966,28 @@ def _kv_desc(cache: dict) -> KvCacheDesc:
                          "[layers, pages, 2, heads, d/32, page]")
     if lens.shape != (seqs,) or refs.shape != (pages,):
         raise ValueError("seq_len has an entry a row of page_table, page_refs one a page")
-    if not (codes.dtype == scales.dtype == torch.uint8
-            and table.dtype == lens.dtype == refs.dtype == torch.int32):
+    if not (codes.dtype is scales.dtype is torch.uint8
+            and table.dtype is lens.dtype is refs.dtype is torch.int32):
         raise ValueError("codes and scales are uint8, page_table, seq_len and page_refs int32")
-    dev = codes.device
     if not (codes.is_contiguous() and scales.is_contiguous() and table.is_contiguous()
-            and lens.is_contiguous() and refs.is_contiguous() and scales.device == dev
-            and table.device == dev and lens.device == dev and refs.device == dev):
-        raise ValueError(f"a cache's tensors must be contiguous and on one device ({dev})")
+            and lens.is_contiguous() and refs.is_contiguous()
+            and codes.get_device() == scales.get_device() == table.get_device()
+            == lens.get_device() == refs.get_device()):
+        raise ValueError(f"a cache's tensors must be contiguous and on one device ({codes.device})")
     if not codes.is_cuda:
-        raise ValueError(f"a cache must be on a GPU (got {dev})")
-    return KvCacheDesc(codes.data_ptr(), scales.data_ptr(), table.data_ptr(), lens.data_ptr(),
-                       refs.data_ptr(), layers, pages, page, heads, 2 * half, seqs, max_pages)
+        raise ValueError(f"a cache must be on a GPU (got {codes.device})")
+    try:
+        return KvCacheDesc.from_buffer_copy(_KV_CACHE_FIELDS.pack(
+            codes.data_ptr(), scales.data_ptr(), table.data_ptr(), lens.data_ptr(),
+            refs.data_ptr(), layers, pages, page, heads, 2 * half, seqs, max_pages))
+    except struct.error:
+        raise ValueError("a cache's sizes are 32-bit numbers") from None
 
 
 def _kv_on(cache: dict, stream, call):
     """call(handle) with the cache's device current and, where a stream is
     named, that stream too, so that what is allocated inside belongs to it."""
-    index = cache["codes"].device.index
+    index = cache["codes"].get_device()
     if stream is None and index == torch._C._cuda_getDevice():
         return call(torch._C._cuda_getCurrentRawStream(index))
     with torch.cuda.device(index):
@@ -1010,7 +1020,8 @@ def _kv_ints(t: torch.Tensor | None, n: int | None, cache: dict, name: str):
     """The address of an int32 tensor of n entries on the cache's device."""
     if t is None:
         return None
-    if (t.dtype != torch.int32 or not t.is_contiguous() or t.device != cache["codes"].device
+    if (t.dtype is not torch.int32 or not t.is_contiguous()
+            or t.get_device() != cache["codes"].get_device()
             or (n is not None and t.numel() != n)):
         raise ValueError(f"{name} must be a contiguous int32 tensor"
                          f"{'' if n is None else f' of {n} entries'} on the cache's device")

@@ -188,3 +188,10 @@ def test_the_binding_refuses_tensors_that_do_not_fit():
             sense.sense_kv_truncate({**kv, name: t})
     with pytest.raises(ValueError):
         sense.sense_build_kv_cache(1, 4, 24, 2, 64, 2, 4, device="cpu")
+
+
+def test_the_binding_packs_a_cache_as_the_header_lays_it_out():
+    fields = sense._KV_CACHE_FIELDS
+    assert fields.size == ctypes.sizeof(sense.KvCacheDesc)
+    got = sense.KvCacheDesc.from_buffer_copy(fields.pack(*range(1, 13)))
+    assert [getattr(got, name) for name, _ in sense.KvCacheDesc._fields_] == list(range(1, 13))
