@@ -733,7 +733,8 @@ __global__ __launch_bounds__(kThreads, MT * D > 128 || MT == 2 ? 2 : (D == 128 ?
 // keys (or their keys or values alone).  Each wave ends with whole rows, so
 // nothing is joined but runs.
 template <int D, bool F16, int MT>
-__global__ __launch_bounds__(kThreads, D >= 128 ? 2 : 3) void kv_many_kernel(Args g) {
+__global__ __launch_bounds__(kThreads, D >= 128 ? 2 : (MT == 1 ? 4 : 3))
+    void kv_many_kernel(Args g) {
     constexpr int kRows = 64 * MT;
     constexpr int kKs = D / 32;
     constexpr int DV = D / 16;
@@ -1171,7 +1172,8 @@ __global__ __launch_bounds__(kThreads) void kv_join_kernel(Args g, int tiles_max
 // of 128: two 2048-token chunks over 6000 positions 356 us, 497 in tiles of 64.
 // Tiles of 64 where the unit has no more, of 256 dims, whose sums take twice
 // the registers, and of 64 dims where they leave a quarter of the rows less
-// empty (183 rows, 16 entries over 2000 positions: 40.9 us, 44.2).
+// empty (183 rows, 16 entries over 200 to 4100 positions: 36.1 us, 39.6 in
+// tiles of 128; all over 2000: 45.7, 45.0; 300 rows, not a quarter: 55.8, 51.8).
 int tile_rows(int max_rows, int group, int d) {
     const int64_t rows = (int64_t)max_rows * group;
     if (rows <= 16) return 16;
@@ -1183,9 +1185,11 @@ int tile_rows(int max_rows, int group, int d) {
 
 // Workgroups to cut the work for: what is resident at once (twice and three
 // times as many took 41 -> 46, 48 us for one token over 131K positions: each
-// costs its start and a partial sum).
+// costs its start and a partial sum; the four that 64-row tiles of 64 dims
+// leave room for against three: 183 rows, 16 entries of 200 to 4100 positions
+// 40.1 -> 36.0 us, all of 2000 45.0 -> 45.4).
 int target_items(int rows, int d) {
-    if (rows > 32) return device_cus() * (d >= 128 ? 2 : 3);
+    if (rows > 32) return device_cus() * (d >= 128 ? 2 : (rows == 64 ? 4 : 3));
     return device_cus() * (rows > 16 || d == 256 ? 2 : (d == 128 ? 3 : 4));
 }
 
