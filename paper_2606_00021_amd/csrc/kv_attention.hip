@@ -41,6 +41,8 @@
 // in its range.  Weights are rounded to the query's type (nearest), which is
 // off by as much as rounding the result is; their sum is taken of the rounded
 // ones, by a product with ones, so that the weights that are used add up to 1.
+#include <type_traits>
+
 #include "internal.h"
 #include "kv.h"
 
@@ -1114,34 +1116,44 @@ __global__ __launch_bounds__(kThreads) void kv_join_kernel(Args g, int tiles_max
         if (on) {
             // The partial sums come from far (other XCDs wrote them): many at
             // a time; places behind the last read the first again, weight 0.
-            constexpr int kEvery = RB == 1 ? kTeams : 1, kBatch = RB == 1 ? 16 : 8;
+            constexpr int kEvery = RB == 1 ? kTeams : 1;
             const int64_t first = ((int64_t)first_item + place) * ROWS + r;
             const int64_t apart = (int64_t)g.c.heads * n_tiles * ROWS;
-            for (int s0 = RB == 1 ? team : 0; s0 < splits; s0 += kBatch * kEvery) {
-                f32x2 ml[kBatch];
-                f32x4 x[kBatch];
+            auto add = [&](auto batch) {
+                constexpr int kBatch = decltype(batch)::value;
+                for (int s0 = RB == 1 ? team : 0; s0 < splits; s0 += kBatch * kEvery) {
+                    f32x2 ml[kBatch];
+                    f32x4 x[kBatch];
 #pragma unroll
-                for (int i = 0; i < kBatch; ++i) {
-                    const int s = s0 + i * kEvery;
-                    const int64_t at = first + (s < splits ? s : s0) * apart;
-                    ml[i] = g.part_ml[at];
-                    x[i] = *(const f32x4*)(g.part_o + at * D + dim);
+                    for (int i = 0; i < kBatch; ++i) {
+                        const int s = s0 + i * kEvery;
+                        const int64_t at = first + (s < splits ? s : s0) * apart;
+                        ml[i] = g.part_ml[at];
+                        x[i] = *(const f32x4*)(g.part_o + at * D + dim);
+                    }
+                    // Left alone, most of the loads are moved behind the
+                    // exponentials, one after the other.
+                    __builtin_amdgcn_sched_barrier(0);
+                    float now = top;
+#pragma unroll
+                    for (int i = 0; i < kBatch; ++i) now = fmaxf(now, ml[i][0]);
+                    const float a = fade(top, now, cs);
+                    l *= a;
+                    sum *= a;
+#pragma unroll
+                    for (int i = 0; i < kBatch; ++i) {
+                        float w = fade(ml[i][0], now, cs);
+                        w = s0 + i * kEvery < splits ? w : 0.f;
+                        l += ml[i][1] * w;
+                        sum += x[i] * w;
+                    }
+                    top = now;
                 }
-                float now = top;
-#pragma unroll
-                for (int i = 0; i < kBatch; ++i) now = fmaxf(now, ml[i][0]);
-                const float a = fade(top, now, cs);
-                l *= a;
-                sum *= a;
-#pragma unroll
-                for (int i = 0; i < kBatch; ++i) {
-                    float w = fade(ml[i][0], now, cs);
-                    w = s0 + i * kEvery < splits ? w : 0.f;
-                    l += ml[i][1] * w;
-                    sum += x[i] * w;
-                }
-                top = now;
-            }
+            };
+            if (splits > 4 * kEvery)
+                add(std::integral_constant<int, RB == 1 ? 16 : 8>());
+            else
+                add(std::integral_constant<int, 4>());
         }
         if constexpr (RB == 1) {
             s_o[team][threadIdx.x % kLanes] = sum;
