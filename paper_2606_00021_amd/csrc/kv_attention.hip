@@ -316,6 +316,22 @@ __device__ __forceinline__ uint32_t pack(float a, float b) {
         return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2));
 }
 
+// The two numbers of a pair.
+template <bool F16>
+__device__ __forceinline__ float low(uint32_t w) {
+    if constexpr (F16)
+        return (float)__builtin_bit_cast(_Float16, (uint16_t)w);
+    else
+        return __builtin_bit_cast(float, w << 16);
+}
+template <bool F16>
+__device__ __forceinline__ float high(uint32_t w) {
+    if constexpr (F16)
+        return (float)__builtin_bit_cast(_Float16, (uint16_t)(w >> 16));
+    else
+        return __builtin_bit_cast(float, w & 0xFFFF0000u);
+}
+
 // Whether a weight of the lane's row, in any of its four lanes, is beyond
 // `limit`.  A row takes a new reference only then, so that its result does not
 // depend on the rows that it shares a wave with.
@@ -595,12 +611,19 @@ __global__ __launch_bounds__(kThreads, MT * D > 128 || MT == 2 ? 2 : (D == 128 ?
                 lsum[mt] *= keep;
             }
         }
-        u32x4 pf[MT];
+        // Weights as the sum of two numbers of the type.
+        u32x4 pf[MT], pl[MT];
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) pf[mt][i] = pack<F16>(w[mt][2 * i], w[mt][2 * i + 1]);
+            for (int i = 0; i < 4; ++i) {
+                const float a = w[mt][2 * i], b = w[mt][2 * i + 1];
+                const uint32_t hi = pack<F16>(a, b);
+                pf[mt][i] = hi;
+                pl[mt][i] = pack<F16>(a - low<F16>(hi), b - high<F16>(hi));
+            }
             lsum[mt] = mfma<F16>(ones, pf[mt], lsum[mt]);
+            lsum[mt] = mfma<F16>(ones, pl[mt], lsum[mt]);
         }
         // V^T: dims DV m + t of the lane's 8 keys.
         float unit[8];
@@ -656,6 +679,8 @@ __global__ __launch_bounds__(kThreads, MT * D > 128 || MT == 2 ? 2 : (D == 128 ?
                 for (int mt = 0; mt < MT; ++mt) {
                     o[t][mt] = mfma<F16>(lo, pf[mt], o[t][mt]);
                     o[t + 1][mt] = mfma<F16>(hi, pf[mt], o[t + 1][mt]);
+                    o[t][mt] = mfma<F16>(lo, pl[mt], o[t][mt]);
+                    o[t + 1][mt] = mfma<F16>(hi, pl[mt], o[t + 1][mt]);
                 }
             }
         }
