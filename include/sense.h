@@ -753,7 +753,8 @@ sense_status_t sense_kv_attention_workspace_size(const sense_kv_cache_t *cache, 
  * touch it, whatever they hold.  Statistics and sums are fp32; cached values
  * enter in q_dtype (exact in BF16 for all that sense_kv_write writes; F16 has
  * to hold them: a row that sees a block of a scale above 2^13 is unspecified),
- * weights are rounded to q_dtype.  NaN that a row sees makes it NaN: a key's
+ * weights are rounded to q_dtype where max_rows * n_heads / n_kv_heads is
+ * above 64, and carry twice its bits up to there.  NaN that a row sees makes it NaN: a key's
  * the whole row, a value's the dims of its block.
  *   q, out      rows of n_heads x head_dim elements of q_dtype (F16, BF16),
  *               head h at h * head_dim; strides in elements; bases and strides

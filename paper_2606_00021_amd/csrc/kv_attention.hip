@@ -38,9 +38,11 @@
 // A key tile lies in one page, so every load has a base that is the same for
 // the wave and an offset that is the same for all steps.
 // 4-bit values times their scales are exact in bf16, and in f16 where they lie
-// in its range.  Weights are rounded to the query's type (nearest), which is
-// off by as much as rounding the result is; their sum is taken of the rounded
-// ones, by a product with ones, so that the weights that are used add up to 1.
+// in its range.  Weights of units of up to 64 rows enter as the sum of two
+// numbers of the query's type, so that only the result is rounded; of larger
+// ones, which the matrix units bound, they are rounded once (nearest), which is
+// off by as much as rounding the result is.  Their sum is taken of what enters,
+// by a product with ones, so that the weights that are used add up to 1.
 #include <type_traits>
 
 #include "internal.h"
@@ -821,6 +823,10 @@ __global__ __launch_bounds__(kThreads, D >= 128 ? 2 : (MT == 1 ? 4 : 3))
         end = own < key1 ? own : key1;
     }
     if (w0 / g.group >= p.rows) end = 0;        // no rows: the wave only widens
+    // Weights as two numbers where a unit has no more rows than this: 48 rows
+    // over 200 to 4100 positions 26.1 -> 28.3 us; 183 rows would pay 35.0 -> 39.5,
+    // two 2048-token chunks 352 -> 446.
+    const bool two = g.b.max_rows * g.group <= 64;
 
     f32x4 o[DV][MT];
     f32x4 lsum[MT];
@@ -1028,6 +1034,22 @@ __global__ __launch_bounds__(kThreads, D >= 128 ? 2 : (MT == 1 ? 4 : 3))
 #pragma unroll
                     for (int mt = 0; mt < MT; ++mt)
                         o[d0 + t][mt] = mfma<F16>(vf[t], pf[mt], o[d0 + t][mt]);
+            }
+            if constexpr (MT == 1) {
+                if (two) {
+                    u32x4 pl;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const uint32_t hi = pf[0][i];
+                        const f32x4 w = s[0][2 * step + (i >> 1)];
+                        pl[i] = pack<F16>(w[2 * i & 3] - low<F16>(hi),
+                                          w[(2 * i & 3) + 1] - high<F16>(hi));
+                    }
+                    lsum[0] = mfma<F16>(ones, pl, lsum[0]);
+#pragma unroll
+                    for (int t = 0; t < DV; ++t)
+                        o[t][0] = mfma<F16>(s_v[buf][t0 / 2 + step][t][lane], pl, o[t][0]);
+                }
             }
             if (flags & (0xA << (4 * step))) {
                 const u32x4 nan = s_nan[buf][t0 / 2 + step][lane];
