@@ -18,7 +18,7 @@
 // (kv_many_kernel).
 //
 // Few rows are bound by the bytes of the cache: 64 streams of 8000 positions
-// (32 / 8 heads of 128, 557 MB) take 109 us, 5.1 TB/s, where a plain read of as
+// (32 / 8 heads of 128, 557 MB) take 111 us, 5.0 TB/s, where a plain read of as
 // many bytes takes 80.  Many rows are bound by the matrix and vector units
 // (exponentials): two 2048-token chunks over 6000 positions 356 us, 937
 // TFLOP/s, where a large bf16 product of the library reaches 1170.

@@ -4,7 +4,8 @@ Bound of one output value, with u the half step of q's type (bf16 2^-8,
 f16 2^-11), o the exact value and spread = sum w |v - o| / sum w:
   u |o|                 the output's own rounding
   u spread              every weight is rounded once, and normalised by the sum
-                        of the rounded ones
+                        of the rounded ones (u^2 spread where it is the sum of
+                        two numbers, the second the first one's rounding)
   2 ds spread           scores off by ds at most change weights by a factor
                         within 1 +- 2 ds (ds < 1/4); a score is a sum of d
                         products in fp32 and one product with the scale:
@@ -28,7 +29,7 @@ from paper_2606_00021_amd import sense
 pytestmark = pytest.mark.gpu
 
 
-def reference(q, kv, scale, see):
+def reference(q, kv, scale, see, once=True):
     """Exact values and bounds; q [m, heads, d] tensor, kv [2, L, kv_heads, d]
     float64, see [m, L] bool."""
     m, heads, d = q.shape
@@ -58,7 +59,7 @@ def reference(q, kv, scale, see):
             assert (ds < 0.25).all()
             big = v.abs().amax() if n else 0.0
             out[:, g] = o
-            tol[:, g] += (u * o.abs() + (u + 2 * ds) * spread
+            tol[:, g] += (u * o.abs() + ((u if once else u * u) + 2 * ds) * spread
                           + ((n + 8) * 2.0 ** -23 + n * 2.0 ** -30) * big)
     return out, tol
 
@@ -464,3 +465,20 @@ def test_scores_beyond_what_their_differences_resolve(dtype, d, rows, heads):
                     tol = u * ref.abs() + 2.0 ** -25 + (n + 8) * 2.0 ** -23 * np.abs(v).max()
                     off = (out[i, j, h] - ref).abs()
                     assert (off <= tol).all(), (scale, i, h, j, float((off / tol).max()))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("d,rows,heads,kv", [(64, 1, 6, 2), (128, 4, 8, 2), (128, 3, 16, 2),
+                                             (256, 2, 4, 1), (64, 9, 14, 2), (128, 16, 4, 1),
+                                             (256, 7, 8, 2)])
+def test_units_of_few_rows_round_only_the_result(dtype, d, rows, heads, kv):
+    """Up to 64 rows of a key head: weights are sums of two numbers."""
+    print(f"[kv attention] two numbers {dtype} d={d} rows={rows}", flush=True)
+    rng = np.random.default_rng(d + rows + heads)
+    lens = [1400, 300, 77]
+    kvc, m = pair(rng, lens, page=32, heads=kv, d=d)
+    q = queries(rng, (3, rows, heads, d), dtype)
+    out = sense.sense_kv_attention(kvc, 0, q).double().cpu()
+    for i, n in enumerate(lens):
+        ref, tol = reference(q[i], m.rows(0, i, 0, n), d ** -0.5, sees(rows, n), once=False)
+        assert ((out[i] - ref).abs() <= tol).all(), (i, float(((out[i] - ref).abs() / tol).max()))
