@@ -342,27 +342,37 @@ __device__ __forceinline__ bool row_over(uint32_t most, uint32_t limit) {
     return (over | over >> 16 | over >> 32 | over >> 48) >> (threadIdx.x & 15) & 1;
 }
 
-// Weights of a row with the reference `now` (a score): 2^(cs (s - now) + lift),
-// computed as fma(s - sub, cs, add).  The step's one fma (sub 0, add = neg) is
-// off by a factor 2^r, r the rounding of cs now, which cancels in the row but
-// leaves the types of weights from cs now = 2^28 on.  Such rows, and those that
-// have seen nothing, have neg infinite, so that each step comes back here.
+// The exponent of the weight of a row's reference, and the bits of the largest
+// weight that leaves the reference as it is: f16 weights up to 2^15, not 2^8.
+constexpr float lift_of(bool f16) { return f16 ? 7.f : 0.f; }
+constexpr uint32_t most_bits(bool f16) { return (uint32_t)(127 + (f16 ? 15 : 8)) << 23; }
+
+// Weights of a row with the reference `now` (a score): 2^(cs s + neg), one fma,
+// neg = lift - cs now rounded once.  What neg is off by is a factor of all
+// weights of this reference; surplus() is its exponent, which is taken out where
+// sums of different references meet.  From cs now = 2^24 on, where it passes 1,
+// weights are 2^(cs (s - now) + lift) instead; such rows, and those that have
+// seen nothing, have neg infinite in the step, so that each step comes back here.
 struct Exponent {
-    float sub, add, neg;
+    float sub, add, neg;                // 2^(cs (s - sub) + add); neg for the step
 };
 __device__ __forceinline__ Exponent exponent(float now, float cs, float lift) {
-    const float at = now * cs;
-    const bool none = now == -INFINITY, far = !none && fabsf(at) >= 0x1p24f;
+    const bool none = now == -INFINITY, far = !none && fabsf(now * cs) >= 0x1p24f;
     Exponent x;
     x.sub = far ? now : 0.f;
-    x.add = none || far ? lift : lift - at;
+    x.add = none || far ? lift : fmaf(-now, cs, lift);
     x.neg = none || far ? INFINITY : x.add;
     return x;
 }
-// What sums of reference `was` are worth at the reference `now`.  A row that
-// has seen nothing has sums of 0 (or of NaN scores).
-__device__ __forceinline__ float fade(float was, float now, float cs) {
-    return was == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((was - now) * cs);
+__device__ __forceinline__ float surplus(float now, float cs, float lift) {
+    const bool exact = now == -INFINITY || fabsf(now * cs) >= 0x1p24f;
+    return exact ? 0.f : fmaf(now, cs, fmaf(-now, cs, lift)) - lift;
+}
+// What sums of reference `was` are worth at the reference `now`, `more` the
+// difference of their surpluses.  A row that has seen nothing has sums of 0 (or
+// of NaN scores).
+__device__ __forceinline__ float fade(float was, float now, float cs, float more = 0.f) {
+    return was == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(fmaf(was - now, cs, more));
 }
 
 __device__ __forceinline__ float unit_of(uint32_t byte) {
@@ -431,6 +441,7 @@ __global__ __launch_bounds__(kThreads, MT * D > 128 || MT == 2 ? 2 : (D == 128 ?
     __shared__ float s_o[kWaves][kRows][kPad];
     __shared__ float s_m[kWaves][kRows];
     __shared__ float s_l[kWaves][kRows];
+    __shared__ float s_more[kWaves][kRows];
 
     const Plan p = plan<kRows>(g);
     if (p.entry < 0) return;
@@ -477,8 +488,8 @@ __global__ __launch_bounds__(kThreads, MT * D > 128 || MT == 2 ? 2 : (D == 128 ?
     f32x4 lsum[MT];
     f32x4 hit[MT];                      // NaN values that a row sees, for its dims
     float ref[MT], neg[MT];             // reference of the weights, see exponent()
-    constexpr float kLift = F16 ? 7.f : 0.f;    // f16: weights up to 2^15, not 2^8
-    constexpr uint32_t kMostBits = (uint32_t)(127 + (F16 ? 15 : 8)) << 23;
+    constexpr float kLift = lift_of(F16);
+    constexpr uint32_t kMostBits = most_bits(F16);
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
 #pragma unroll
@@ -600,7 +611,8 @@ __global__ __launch_bounds__(kThreads, MT * D > 128 || MT == 2 ? 2 : (D == 128 ?
                 now = fmaxf(now, __shfl_xor(now, 16));
                 now = fmaxf(fmaxf(now, __shfl_xor(now, 32)), ref[mt]);
                 now = row_over(most[mt], kMostBits) ? now : ref[mt];
-                const float keep = fade(ref[mt], now, cs);
+                const float keep = fade(
+                    ref[mt], now, cs, surplus(now, cs, kLift) - surplus(ref[mt], cs, kLift));
                 const Exponent x = exponent(now, cs, kLift);
                 ref[mt] = now;
                 neg[mt] = x.neg;
@@ -714,6 +726,7 @@ __global__ __launch_bounds__(kThreads, MT * D > 128 || MT == 2 ? 2 : (D == 128 ?
         if (grp == 0) {
             s_m[wave][r] = ref[mt];
             s_l[wave][r] = lsum[mt][0];
+            s_more[wave][r] = surplus(ref[mt], cs, kLift);
         }
 #pragma unroll
         for (int q = 0; q < 4; ++q)
@@ -736,7 +749,7 @@ __global__ __launch_bounds__(kThreads, MT * D > 128 || MT == 2 ? 2 : (D == 128 ?
         f32x4 sum = {0, 0, 0, 0};
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) {
-            const float f = fade(s_m[w][r], top, cs);
+            const float f = fade(s_m[w][r], top, cs, -s_more[w][r]);
             l += s_l[w][r] * f;
             sum += *(const f32x4*)&s_o[w][r][dim] * f;
         }
@@ -832,8 +845,8 @@ __global__ __launch_bounds__(kThreads, D >= 128 ? 2 : (MT == 1 ? 4 : 3))
     f32x4 lsum[MT];
     f32x4 hit[MT];
     float ref[MT], neg[MT];
-    constexpr float kLift = F16 ? 7.f : 0.f;
-    constexpr uint32_t kMostBits = (uint32_t)(127 + (F16 ? 15 : 8)) << 23;
+    constexpr float kLift = lift_of(F16);
+    constexpr uint32_t kMostBits = most_bits(F16);
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
 #pragma unroll
@@ -996,7 +1009,8 @@ __global__ __launch_bounds__(kThreads, D >= 128 ? 2 : (MT == 1 ? 4 : 3))
                 now = fmaxf(now, __shfl_xor(now, 16));
                 now = fmaxf(fmaxf(now, __shfl_xor(now, 32)), ref[mt]);
                 now = row_over(most[mt], kMostBits) ? now : ref[mt];
-                const float keep = fade(ref[mt], now, cs);
+                const float keep = fade(
+                    ref[mt], now, cs, surplus(now, cs, kLift) - surplus(ref[mt], cs, kLift));
                 const Exponent x = exponent(now, cs, kLift);
                 ref[mt] = now;
                 neg[mt] = x.neg;
@@ -1119,14 +1133,15 @@ __global__ __launch_bounds__(kThreads, D >= 128 ? 2 : (MT == 1 ? 4 : 3))
             }
         } else {
             float* dst = g.part_o + ((int64_t)p.item * kRows + r) * D + 4 * DV * grp;
+            const float less = __builtin_amdgcn_exp2f(-surplus(ref[mt], cs, kLift));
 #pragma unroll
             for (int at = 0; at < 4 * DV; at += 4) {
                 const int q = at / DV, t = at % DV;
                 *(f32x4*)(dst + at) =
-                    f32x4{o[t][mt][q], o[t + 1][mt][q], o[t + 2][mt][q], o[t + 3][mt][q]} +
+                    f32x4{o[t][mt][q], o[t + 1][mt][q], o[t + 2][mt][q], o[t + 3][mt][q]} * less +
                     (hit[mt][q] > 0.f ? NAN : 0.f);
             }
-            if (grp == 0) g.part_ml[(int64_t)p.item * kRows + r] = f32x2{ref[mt], l};
+            if (grp == 0) g.part_ml[(int64_t)p.item * kRows + r] = f32x2{ref[mt], l * less};
         }
     }
 }
