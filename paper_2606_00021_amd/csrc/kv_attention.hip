@@ -38,11 +38,14 @@
 // A key tile lies in one page, so every load has a base that is the same for
 // the wave and an offset that is the same for all steps.
 // 4-bit values times their scales are exact in bf16, and in f16 where they lie
-// in its range.  Weights of units of up to 64 rows enter as the sum of two
-// numbers of the query's type, so that only the result is rounded; of larger
-// ones, which the matrix units bound, they are rounded once (nearest), which is
-// off by as much as rounding the result is.  Their sum is taken of what enters,
-// by a product with ones, so that the weights that are used add up to 1.
+// in its range.  Weights of entries of up to 64 rows enter as the sum of two
+// numbers of 16 bits, so that only the result is rounded.  Of larger ones, which
+// the matrix units bound, they are rounded once (nearest), to f16 whatever the
+// query's type: 11 bits, so a bf16 result is off by its own rounding and 1 % more
+// (weights of 8 bits: 40 %), an f16 one by 40 % more.  Values then enter in f16;
+// the few that it does not hold in bf16 beside it (kv_many_kernel).  The weights'
+// sum is taken of what enters, by a product with ones, so that the weights that
+// are used add up to 1.
 #include <type_traits>
 
 #include "internal.h"
@@ -383,6 +386,15 @@ __device__ __forceinline__ float unit_of(uint32_t byte) {
 template <bool F16>
 __device__ __forceinline__ float finite_unit(float unit) {
     return fminf(unit, F16 ? 0x1p13f : 0x1p125f);
+}
+
+// Codes of a scale byte that f16 does not hold: units of 2^-23 to 2^13 it does,
+// and zeros of any.  (A NaN block has no values.)
+template <int N>
+__device__ __forceinline__ bool beyond_f16(uint32_t byte, const uint32_t (&codes)[N]) {
+    uint32_t some = codes[0];
+    if constexpr (N == 2) some |= codes[1];
+    return byte - 104u > 36u && byte != 255u && (some & 0x77777777u) != 0;
 }
 
 // Which of 4 N positions a row sees: bit 4t + r is position first + 16t + r,
@@ -774,6 +786,13 @@ __global__ __launch_bounds__(kThreads, MT * D > 128 || MT == 2 ? 2 : (D == 128 ?
 // in turn, so that one is read while the next is written; a wave widens 16
 // keys (or their keys or values alone).  Each wave ends with whole rows, so
 // nothing is joined but runs.
+//
+// Keys are widened to the query's type, values to f16.  A part with a scale
+// outside 2^-19 .. 2^12 (one test of four bytes) is looked at value by value: what
+// f16 does not hold is 0 in LDS, and each wave fetches it again in bf16, for
+// products of its own.  Two 2048-token chunks take 339 us, as with weights and
+// values in bf16 (344; with values of both kinds in LDS and a mask: 391).  Where
+// every value is beyond f16 they take 2.8 times as long.
 template <int D, bool F16, int MT>
 __global__ __launch_bounds__(kThreads, D >= 128 ? 2 : (MT == 1 ? 4 : 3))
     void kv_many_kernel(Args g) {
@@ -782,11 +801,10 @@ __global__ __launch_bounds__(kThreads, D >= 128 ? 2 : (MT == 1 ? 4 : 3))
     constexpr int DV = D / 16;
     constexpr int KT = D == 256 ? 32 : 64;          // keys of a tile
     constexpr int kTiles = 2;                       // parts of 16 keys worked on at a time
-    constexpr int kSteps = kTiles / 2;
     __shared__ u32x4 s_k[2][KT / 16][kKs][64];
     __shared__ u32x4 s_v[2][KT / 32][DV][64];
     __shared__ u32x4 s_nan[2][KT / 32][64]; // 1 where a value is NaN
-    __shared__ int s_flag[2][KT / 16];      // 1: no page, 2: some value is NaN
+    __shared__ int s_flag[2][KT / 16];      // 1: no page, 2: some value is NaN, 4: some beyond f16
 
     const Plan p = plan<kRows>(g);
     if (p.entry < 0) return;
@@ -836,17 +854,17 @@ __global__ __launch_bounds__(kThreads, D >= 128 ? 2 : (MT == 1 ? 4 : 3))
         end = own < key1 ? own : key1;
     }
     if (w0 / g.group >= p.rows) end = 0;        // no rows: the wave only widens
-    // Weights as two numbers where a unit has no more rows than this: 48 rows
-    // over 200 to 4100 positions 26.1 -> 28.3 us; 183 rows would pay 35.0 -> 39.5,
-    // two 2048-token chunks 352 -> 446.
-    const bool two = g.b.max_rows * g.group <= 64;
+    // Weights as two numbers where the entry has no more rows than this, whatever
+    // lies beside it: 48 rows over 200 to 4100 positions 26.1 -> 28.3 us; 183 rows
+    // would pay 35.0 -> 39.5, two 2048-token chunks 352 -> 446.
+    const bool two = p.rows * g.group <= 64;
 
     f32x4 o[DV][MT];
     f32x4 lsum[MT];
     f32x4 hit[MT];
     float ref[MT], neg[MT];
-    constexpr float kLift = lift_of(F16);
-    constexpr uint32_t kMostBits = most_bits(F16);
+    constexpr float kLift = lift_of(true);
+    constexpr uint32_t kMostBits = most_bits(true);
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
 #pragma unroll
@@ -857,7 +875,7 @@ __global__ __launch_bounds__(kThreads, D >= 128 ? 2 : (MT == 1 ? 4 : 3))
         neg[mt] = INFINITY;
     }
     const float cs = g.a.scale * 1.4426950408889634f;
-    const uint32_t one = F16 ? 0x3C003C00u : 0x3F803F80u;
+    constexpr uint32_t one = 0x3C003C00u;
     const u32x4 ones = {one, one, one, one};
 
     const ScalarInts table =
@@ -872,6 +890,23 @@ __global__ __launch_bounds__(kThreads, D >= 128 ? 2 : (MT == 1 ? 4 : 3))
     const bool do_k = KT == 64 || (wave & 1) == 0, do_v = KT == 64 || (wave & 1) == 1;
     uint32_t rk[D / 32], rks[D == 256 ? 2 : 1], rv[4][D == 256 ? 2 : 1], rvs;
     int bad = 0;
+    typedef uint32_t Codes[4][D == 256 ? 2 : 1];
+    auto load_v = [&](int id, int slot, Codes& codes, uint32_t& bytes) {
+        const int64_t vr = id * page_rows + v_rows;
+        const uint8_t* vc = g.c.codes + (vr + slot) * (D / 2) + 4 * grp * (D / 2) + col * (D / 32);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (D == 64) {
+                codes[i][0] = *(const uint16_t*)(vc + i * (D / 2));
+            } else {
+#pragma unroll
+                for (int w = 0; w < D / 128; ++w)
+                    codes[i][w] = ((const uint32_t*)(vc + i * (D / 2)))[w];
+            }
+        }
+        bytes = *(const uint32_t*)(g.c.scales + vr * (D / 32) + slot + 4 * grp +
+                                   ((col * DV / 32) << lg));
+    };
     auto fetch = [&](int key) {
         int id = key + 16 * part < p.len ? table[(key + 16 * part) >> lg] : -1;
         bad = !kv_page_ok(g.c, id);
@@ -887,23 +922,7 @@ __global__ __launch_bounds__(kThreads, D >= 128 ? 2 : (MT == 1 ? 4 : 3))
 #pragma unroll
             for (int w = 0; w < (D == 256 ? 2 : 1); ++w) rks[w] = ks[w << lg];
         }
-        if (do_v) {
-            const int64_t vr = id * page_rows + v_rows;
-            const uint8_t* vc =
-                g.c.codes + (vr + slot) * (D / 2) + 4 * grp * (D / 2) + col * (D / 32);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if constexpr (D == 64) {
-                    rv[i][0] = *(const uint16_t*)(vc + i * (D / 2));
-                } else {
-#pragma unroll
-                    for (int w = 0; w < D / 128; ++w)
-                        rv[i][w] = ((const uint32_t*)(vc + i * (D / 2)))[w];
-                }
-            }
-            rvs = *(const uint32_t*)(g.c.scales + vr * (D / 32) + slot + 4 * grp +
-                                     ((col * DV / 32) << lg));
-        }
+        if (do_v) load_v(id, slot, rv, rvs);
     };
     auto spread = [&](int buf) {
         if (do_k) {
@@ -912,21 +931,29 @@ __global__ __launch_bounds__(kThreads, D >= 128 ? 2 : (MT == 1 ? 4 : 3))
                 s_k[buf][part][q][lane] = widen8<F16>(rk[q], unit_of(rks[D == 256 ? q >> 2 : 0]));
         }
         if (do_v) {
-            float unit[4];
-            bool some = false;
-            uint32_t nan[2] = {0, 0};
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint32_t byte = (rvs >> (8 * i)) & 0xFFu;
-                const bool here = byte == 255u;
-                some |= here;
-                nan[i >> 1] |= here ? (i & 1 ? one & 0xFFFF0000u : one & 0xFFFFu) : 0u;
-                unit[i] = here ? 0.f : finite_unit<F16>(unit_of(byte));
-            }
             const int step = part >> 1, half = part & 1;
-            const bool any = __any(some);
-            if (lane == 0) s_flag[buf][part] = bad | (any ? 2 : 0);
-            ((u32x2*)&s_nan[buf][step][lane])[half] = u32x2{nan[0], nan[1]};
+            float unit[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) unit[i] = unit_of((rvs >> (8 * i)) & 0xFFu);
+            int flag = bad;
+            // All four scales 108 to 139: finite in f16.  Where the sum carries, a
+            // byte of 236 or more shows itself.
+            if (__any(((rvs + 0x14141414u) & 0xE0E0E0E0u) != 0x80808080u)) {
+                uint32_t nan[2] = {0, 0};
+                bool some = false, odd = false;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t byte = (rvs >> (8 * i)) & 0xFFu;
+                    const bool here = byte == 255u, out = !F16 && beyond_f16(byte, rv[i]);
+                    some |= here;
+                    odd |= out;
+                    nan[i >> 1] |= here ? (i & 1 ? one & 0xFFFF0000u : one & 0xFFFFu) : 0u;
+                    unit[i] = here || out ? 0.f : finite_unit<true>(unit[i]);
+                }
+                flag |= (__any(some) ? 2 : 0) | (__any(odd) ? 4 : 0);
+                ((u32x2*)&s_nan[buf][step][lane])[half] = u32x2{nan[0], nan[1]};
+            }
+            if (lane == 0) s_flag[buf][part] = flag;
 #pragma unroll
             for (int w = 0; w < (D == 256 ? 2 : 1); ++w)
 #pragma unroll
@@ -934,10 +961,10 @@ __global__ __launch_bounds__(kThreads, D >= 128 ? 2 : (MT == 1 ? 4 : 3))
                     uint32_t x[4];
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
-                        x[i] = by == 0   ? widen<F16, 0>(rv[i][w], unit[i])
-                               : by == 1 ? widen<F16, 1>(rv[i][w], unit[i])
-                               : by == 2 ? widen<F16, 2>(rv[i][w], unit[i])
-                                         : widen<F16, 3>(rv[i][w], unit[i]);
+                        x[i] = by == 0   ? widen<true, 0>(rv[i][w], unit[i])
+                               : by == 1 ? widen<true, 1>(rv[i][w], unit[i])
+                               : by == 2 ? widen<true, 2>(rv[i][w], unit[i])
+                                         : widen<true, 3>(rv[i][w], unit[i]);
                     const int t = 8 * w + 2 * by;
                     ((u32x2*)&s_v[buf][step][t][lane])[half] =
                         u32x2{__builtin_amdgcn_perm(x[1], x[0], 0x05040100u),
@@ -956,7 +983,7 @@ __global__ __launch_bounds__(kThreads, D >= 128 ? 2 : (MT == 1 ? 4 : 3))
         if (!plain) {
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt)
-                vis[mt] = seen_bits<kTiles>(g, p, tok[mt], key + 4 * grp, key1, flags, 2);
+                vis[mt] = seen_bits<kTiles>(g, p, tok[mt], key + 4 * grp, key1, flags, 3);
         }
         f32x4 s[MT][kTiles];
         auto scores = [&]() {
@@ -1023,60 +1050,120 @@ __global__ __launch_bounds__(kThreads, D >= 128 ? 2 : (MT == 1 ? 4 : 3))
                 lsum[mt] *= keep;
             }
         }
+        const int at = t0 / 2;
+        constexpr int kBatch = DV < 8 ? DV : 8;
+        u32x4 pf[MT];
 #pragma unroll
-        for (int step = 0; step < kSteps; ++step) {
-            constexpr int kBatch = DV < 8 ? DV : 8;
-            u32x4 pf[MT];
+        for (int d0 = 0; d0 < DV; d0 += kBatch) {
+            u32x4 vf[kBatch];
 #pragma unroll
-            for (int d0 = 0; d0 < DV; d0 += kBatch) {
-                u32x4 vf[kBatch];
-#pragma unroll
-                for (int t = 0; t < kBatch; ++t) vf[t] = s_v[buf][t0 / 2 + step][d0 + t][lane];
-                __builtin_amdgcn_sched_barrier(0);
-                if (d0 == 0) {
-#pragma unroll
-                    for (int mt = 0; mt < MT; ++mt) {
-#pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            pf[mt][i] = pack<F16>(s[mt][2 * step + (i >> 1)][2 * i & 3],
-                                                  s[mt][2 * step + (i >> 1)][(2 * i & 3) + 1]);
-                        lsum[mt] = mfma<F16>(ones, pf[mt], lsum[mt]);
-                    }
-                }
-#pragma unroll
-                for (int t = 0; t < kBatch; ++t)
-#pragma unroll
-                    for (int mt = 0; mt < MT; ++mt)
-                        o[d0 + t][mt] = mfma<F16>(vf[t], pf[mt], o[d0 + t][mt]);
-            }
-            if constexpr (MT == 1) {
-                if (two) {
-                    u32x4 pl;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const uint32_t hi = pf[0][i];
-                        const f32x4 w = s[0][2 * step + (i >> 1)];
-                        pl[i] = pack<F16>(w[2 * i & 3] - low<F16>(hi),
-                                          w[(2 * i & 3) + 1] - high<F16>(hi));
-                    }
-                    lsum[0] = mfma<F16>(ones, pl, lsum[0]);
-#pragma unroll
-                    for (int t = 0; t < DV; ++t)
-                        o[t][0] = mfma<F16>(s_v[buf][t0 / 2 + step][t][lane], pl, o[t][0]);
-                }
-            }
-            if (flags & (0xA << (4 * step))) {
-                const u32x4 nan = s_nan[buf][t0 / 2 + step][lane];
+            for (int t = 0; t < kBatch; ++t) vf[t] = s_v[buf][at][d0 + t][lane];
+            __builtin_amdgcn_sched_barrier(0);
+            if (d0 == 0) {
 #pragma unroll
                 for (int mt = 0; mt < MT; ++mt) {
-                    const uint32_t v = vis[mt] >> (8 * step);
-                    u32x4 seen;
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
-                        seen[i] = (v >> (2 * i) & 1 ? one & 0xFFFFu : 0u) |
-                                  (v >> (2 * i + 1) & 1 ? one & 0xFFFF0000u : 0u);
-                    hit[mt] = mfma<F16>(nan, seen, hit[mt]);
+                        pf[mt][i] =
+                            pack<true>(s[mt][i >> 1][2 * i & 3], s[mt][i >> 1][(2 * i & 3) + 1]);
+                    lsum[mt] = mfma<true>(ones, pf[mt], lsum[mt]);
                 }
+            }
+#pragma unroll
+            for (int t = 0; t < kBatch; ++t)
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt)
+                    o[d0 + t][mt] = mfma<true>(vf[t], pf[mt], o[d0 + t][mt]);
+        }
+        if (!two && !(flags & 0x36)) return;            // most often
+        // What pf leaves of the weights.
+        u32x4 pl[MT];
+        if (two) {
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t hi = pf[mt][i];
+                    pl[mt][i] = pack<true>(s[mt][i >> 1][2 * i & 3] - low<true>(hi),
+                                           s[mt][i >> 1][(2 * i & 3) + 1] - high<true>(hi));
+                }
+                lsum[mt] = mfma<true>(ones, pl[mt], lsum[mt]);
+            }
+#pragma unroll
+            for (int t = 0; t < DV; ++t)
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt)
+                    o[t][mt] = mfma<true>(s_v[buf][at][t][lane], pl[mt], o[t][mt]);
+        }
+        if (!F16 && (flags & 0x24)) {
+            // Values beyond f16 are 0 in s_v.  They come from the cache again, in
+            // bf16, and meet the same weights: two numbers of bf16 hold one of
+            // f16, a third what pl has.
+            Codes codes[2];
+            float unit[8];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int from = key + 16 * h;
+                const int id = from < p.len ? table[from >> lg] : -1;
+                uint32_t bytes;
+                load_v(kv_page_ok(g.c, id) ? id : 0, from & slot_mask, codes[h], bytes);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t byte = (bytes >> (8 * i)) & 0xFFu;
+                    unit[4 * h + i] = beyond_f16(byte, codes[h][i])
+                                          ? finite_unit<false>(unit_of(byte)) : 0.f;
+                }
+            }
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) {
+                u32x4 p0, p1, p2;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float a = low<true>(pf[mt][i]), b = high<true>(pf[mt][i]);
+                    p0[i] = pack<false>(a, b);
+                    p1[i] = pack<false>(a - low<false>(p0[i]), b - high<false>(p0[i]));
+                    p2[i] = two ? pack<false>(low<true>(pl[mt][i]), high<true>(pl[mt][i])) : 0u;
+                }
+#pragma unroll
+                for (int w = 0; w < (D == 256 ? 2 : 1); ++w)
+#pragma unroll
+                    for (int by = 0; by < (D == 64 ? 2 : 4); ++by) {
+                        uint32_t x[8];
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            const uint32_t word = codes[i >> 2][i & 3][w];
+                            x[i] = by == 0   ? widen<false, 0>(word, unit[i])
+                                   : by == 1 ? widen<false, 1>(word, unit[i])
+                                   : by == 2 ? widen<false, 2>(word, unit[i])
+                                             : widen<false, 3>(word, unit[i]);
+                        }
+#pragma unroll
+                        for (int odd = 0; odd < 2; ++odd) {
+                            u32x4 v;
+#pragma unroll
+                            for (int i = 0; i < 4; ++i)
+                                v[i] = __builtin_amdgcn_perm(x[2 * i + 1], x[2 * i],
+                                                             odd ? 0x07060302u : 0x05040100u);
+                            const int t = 8 * w + 2 * by + odd;
+                            o[t][mt] = mfma<false>(v, p0, o[t][mt]);
+                            o[t][mt] = mfma<false>(v, p1, o[t][mt]);
+                            o[t][mt] = mfma<false>(v, p2, o[t][mt]);
+                        }
+                    }
+            }
+        }
+        if (flags & 0x12) {
+            u32x4 nan = s_nan[buf][at][lane];           // of a half that has none: anything
+#pragma unroll
+            for (int i = 0; i < 4; ++i) nan[i] = flags & (i < 2 ? 2 : 0x10) ? nan[i] : 0u;
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) {
+                u32x4 seen;
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    seen[i] = (vis[mt] >> (2 * i) & 1 ? one & 0xFFFFu : 0u) |
+                              (vis[mt] >> (2 * i + 1) & 1 ? one & 0xFFFF0000u : 0u);
+                hit[mt] = mfma<true>(nan, seen, hit[mt]);
             }
         }
     };
@@ -1088,14 +1175,14 @@ __global__ __launch_bounds__(kThreads, D >= 128 ? 2 : (MT == 1 ? 4 : 3))
         __syncthreads();
         int buf = 0;
         for (int key = key0; key < key1; key += KT) {
-            // Flags of the tile's parts, two bits each.
+            // Flags of the tile's parts, three bits each.
             int flags = 0;
 #pragma unroll
-            for (int t = 0; t < KT / 16; ++t) flags |= s_flag[buf][t] << (2 * t);
+            for (int t = 0; t < KT / 16; ++t) flags |= s_flag[buf][t] << (3 * t);
             flags = __builtin_amdgcn_readfirstlane(flags);
 #pragma unroll
             for (int t0 = 0; t0 < KT / 16; t0 += kTiles) {
-                const int at = key + 16 * t0, part = flags >> (2 * t0) & ((1 << 2 * kTiles) - 1);
+                const int at = key + 16 * t0, part = flags >> (3 * t0) & ((1 << 3 * kTiles) - 1);
                 if (at < end)
                     compute(buf, t0, at, part, at + 16 * kTiles <= full && at + 16 * kTiles <= end &&
                                                    part == 0);
