@@ -686,7 +686,8 @@ typedef struct {
  * (max_rows when NULL; clamped to [0, max_rows]): row j of the entry is row
  * row_start[i] + j of the tensors (i * max_rows + j when NULL) and stands for
  * position seq_len - m + j, the last m positions of the sequence.  Rows outside
- * [0, n_rows), positions below 0 and entries of no sequence are left out; a
+ * [0, n_rows) and entries of no sequence are left out, and by sense_kv_write and
+ * sense_kv_read positions below 0 (sense_kv_attention writes their rows as 0); a
  * row of an output that belongs to two entries is written by either.
  * n <= 65536, 1 <= max_rows <= 2^20; arrays are DEVICE memory. */
 typedef struct {
@@ -749,7 +750,8 @@ sense_status_t sense_kv_attention_workspace_size(const sense_kv_cache_t *cache, 
  *   else        p < base, and p = base + u where
  *               mask[i * mask_stride + j * mask_ld + u] != 0
  * (for a draft tree the mask of sense_build_loose_trie, row_len its tree_len).
- * A row that sees nothing becomes 0.  Positions that a row does not see do not
+ * A row whose own position base + j is below 0 sees nothing, whatever its mask
+ * names.  A row that sees nothing becomes 0.  Positions that a row does not see do not
  * touch it, whatever they hold.  Statistics and sums are fp32; cached values
  * are exact for BF16 queries (all that sense_kv_write writes); for F16 ones F16
  * has to hold them: a row that sees a block of a scale above 2^13 is unspecified.

@@ -398,8 +398,9 @@ __device__ __forceinline__ bool beyond_f16(uint32_t byte, const uint32_t (&codes
 }
 
 // Which of 4 N positions a row sees: bit 4t + r is position first + 16t + r,
-// with `none` the tiles that have no page (bit `stride` t).  The mask's bytes
-// are read together, from places inside it whether they count or not.
+// with `none` the tiles that have no page (bit `stride` t).  A row whose own
+// position would be below 0 sees none.  The mask's bytes are read together, from
+// places inside it whether they count or not.
 template <int N>
 __device__ __forceinline__ uint32_t seen_bits(const Args& g, const Plan& p, int token, int first,
                                               int end, uint32_t none, int stride) {
@@ -422,7 +423,7 @@ __device__ __forceinline__ uint32_t seen_bits(const Args& g, const Plan& p, int 
         if (!g.a.mask)
             see = see && u <= token;
         else
-            see = see && (u < 0 || (byte[e] != 0 && token < p.rows));
+            see = see && (u < 0 || (byte[e] != 0 && token < p.rows && base + token >= 0));
         bits |= (uint32_t)see << e;
     }
     return bits;

@@ -1134,7 +1134,8 @@ def sense_kv_attention(cache: dict, layer: int, q: torch.Tensor, mask: torch.Ten
     first seq_len - m + j + 1 positions, or with ``mask`` (uint8 or bool
     [n, nodes, nodes], nodes >= max_rows: sense_build_loose_trie's) all
     positions in front of the entry's rows and those rows u that
-    mask[i, j, u] names.  ``max_kv`` bounds the sequences' lengths (0: the
+    mask[i, j, u] names; a row in front of the first position sees none and
+    becomes 0.  ``max_kv`` bounds the sequences' lengths (0: the
     capacity); ``softmax_scale`` (in (0, 2^127]) is d**-0.5 by default.  Returns ``out``
     (like q; rows that belong to no entry keep what they hold, so without ``out``
     they hold nothing in particular)."""
