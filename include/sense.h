@@ -791,7 +791,8 @@ sense_status_t sense_kv_truncate(const sense_kv_cache_t *cache, const int32_t *s
 
 /* Let sequence dst[i] hold what src[i] holds, by sharing its pages.  REFUSED:
  * no such sequence, dst[i] is not empty or was listed before, src[i] is some
- * entry's destination.  A source may be listed many times. */
+ * entry's destination.  A source may be listed many times.
+ * Errors: INVALID_ARGUMENT, MISALIGNED, HIP. */
 sense_status_t sense_kv_fork(const sense_kv_cache_t *cache, const int32_t *src,
                              const int32_t *dst, int32_t n, int32_t *out_status, void *stream);
 

@@ -4,6 +4,8 @@
 #include <stdarg.h>
 #include <stdio.h>
 
+#include <initializer_list>
+
 #include "internal.h"
 #include "kv.h"
 #include "sense.h"
@@ -158,6 +160,14 @@ sense_status_t check_entries(const KvCache& c, const int32_t* seqs, int32_t n) {
     return SENSE_OK;
 }
 
+// int32 arrays of a page operation (NULL where one is not given).
+sense_status_t check_ints(const char* names, std::initializer_list<const void*> arrays) {
+    for (const void* p : arrays)
+        if (!aligned(p, 4))
+            return fail(SENSE_ERR_MISALIGNED, "%s are int32 arrays", names);
+    return SENSE_OK;
+}
+
 sense_status_t check_workspace(const void* ws, size_t have, size_t need) {
     if (need == 0) return SENSE_OK;
     if (!ws || have < need)
@@ -278,6 +288,8 @@ SENSE_EXPORT sense_status_t sense_kv_truncate(const sense_kv_cache_t* cache, con
     sense_status_t s = check_cache(cache, &c);
     if (s != SENSE_OK || (s = check_entries(c, seqs, n)) != SENSE_OK) return s;
     if (n == 0) return ok();
+    if ((s = check_ints("seqs, lens and out_status", {seqs, lens, out_status})) != SENSE_OK)
+        return s;
     return launched(sense::launch_kv_truncate(c, seqs, lens, n, out_status, (hipStream_t)stream),
                     "cache truncate");
 }
@@ -293,6 +305,7 @@ SENSE_EXPORT sense_status_t sense_kv_fork(const sense_kv_cache_t* cache, const i
                     sense::kKvMaxEntries);
     if (n == 0) return ok();
     if (!src || !dst) return fail(SENSE_ERR_INVALID_ARGUMENT, "src and dst must be non-NULL");
+    if ((s = check_ints("src, dst and out_status", {src, dst, out_status})) != SENSE_OK) return s;
     return launched(sense::launch_kv_fork(c, src, dst, n, out_status, (hipStream_t)stream),
                     "cache fork");
 }
@@ -318,6 +331,8 @@ SENSE_EXPORT sense_status_t sense_kv_reserve(const sense_kv_cache_t* cache, cons
     if (s != SENSE_OK || (s = check_entries(c, seqs, n)) != SENSE_OK) return s;
     if (n == 0) return ok();
     if (!counts) return fail(SENSE_ERR_INVALID_ARGUMENT, "counts is NULL");
+    if ((s = check_ints("seqs, counts and out_status", {seqs, counts, out_status})) != SENSE_OK)
+        return s;
     if ((s = check_workspace(workspace, workspace_bytes,
                              sense::kv_reserve_workspace_bytes(n, c.n_pages))) != SENSE_OK)
         return s;
@@ -352,6 +367,9 @@ SENSE_EXPORT sense_status_t sense_kv_compact(const sense_kv_cache_t* cache, cons
     if (n == 0) return ok();
     if (!tails || !keep || !keep_len)
         return fail(SENSE_ERR_INVALID_ARGUMENT, "tails, keep and keep_len must be non-NULL");
+    if ((s = check_ints("seqs, tails, keep, keep_len, pick and out_status",
+                        {seqs, tails, keep, keep_len, pick, out_status})) != SENSE_OK)
+        return s;
     if ((int64_t)n * (1 + (int64_t)c.n_layers * 2 * c.heads) / 4 > kMaxBlocks)
         return fail(SENSE_ERR_UNSUPPORTED, "%d entries of %d layers: too many for one call", n,
                     c.n_layers);
