@@ -1,0 +1,127 @@
+"""The cache's attention in runs: calls whose sequences are long enough that
+units are cut and joined, in every kernel and plan.  Each test first shows, by
+the workspace, that the call is cut, and that the call it is compared with is
+not.  Bounds as in test_gpu_kv_attention."""
+import numpy as np
+import pytest
+import torch
+
+from kv_gpu import DEV, ints, pair
+from paper_2606_00021_amd import sense
+from test_gpu_kv_attention import compare, queries
+
+pytestmark = pytest.mark.gpu
+
+
+def bytes_of(kvc, q, max_kv=0):
+    return sense.sense_kv_attention_workspace_size(kvc, q.shape[0], q.shape[1], q.shape[2], max_kv)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("d,heads,kv", [(64, 4, 2), (128, 7, 1), (256, 4, 2), (128, 32, 1),
+                                        (128, 48, 1)])
+def test_tokens_of_more_than_64_streams(dtype, d, heads, kv):
+    """A plan in front (more than 64 entries); long entries among short and
+    empty ones, in the order of the sequences and in another."""
+    print(f"[kv runs] 70 streams {dtype} d={d} {heads}/{kv}", flush=True)
+    rng = np.random.default_rng(d + heads)
+    lens = rng.integers(0, 60, 70).tolist()
+    lens[0], lens[1], lens[33], lens[64], lens[69] = 1500, 0, 2700, 1030, 2049
+    kvc, m = pair(rng, lens, page=32, heads=kv, d=d)
+    q = queries(rng, (70, 1, heads, d), dtype)
+    assert bytes_of(kvc, q) > 2 * bytes_of(kvc, q, 1024)         # partial sums; plans alone
+    at = (0, 1, 2, 33, 63, 64, 65, 69)
+    out = sense.sense_kv_attention(kvc, 0, q)
+    whole = sense.sense_kv_attention(kvc, 0, q, max_kv=1024)     # longer ones all the same
+    for i in at:
+        compare(out[i:i + 1], q[i:i + 1], m, 0, [i], [1])
+        compare(whole[i:i + 1], q[i:i + 1], m, 0, [i], [1])
+    assert torch.equal(out[1], torch.zeros_like(out[1]))
+    order = rng.permutation(70)
+    moved = sense.sense_kv_attention(kvc, 0, q[torch.tensor(order, device=DEV)], seqs=ints(order))
+    for i in at:
+        j = int(np.nonzero(order == i)[0][0])
+        compare(moved[j:j + 1], q[i:i + 1], m, 0, [i], [1])
+    # a listed sequence that is none, and one that is listed twice
+    listed = order.copy()
+    listed[3], listed[4] = -1, order[5]
+    kept = torch.full_like(q, 9)
+    again = sense.sense_kv_attention(kvc, 0, q[torch.tensor(order, device=DEV)],
+                                     seqs=ints(listed), out=kept)
+    assert (again[3] == 9).all() and torch.isfinite(again).all()
+    compare(again[4:5], q[order[4]:order[4] + 1], m, 0, [int(order[5])], [1])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("d,heads,kv", [(64, 2, 2), (128, 8, 1), (256, 20, 1), (64, 32, 1)])
+def test_whole_units_and_runs_agree(dtype, d, heads, kv):
+    """The bound on the lengths decides about the launches, not the values."""
+    print(f"[kv runs] whole {dtype} d={d} {heads}/{kv}", flush=True)
+    rng = np.random.default_rng(d + heads)
+    lens = [1, 1024, 1025, 2050, 300, 5]
+    kvc, m = pair(rng, lens, page=16, heads=kv, d=d)
+    q = queries(rng, (6, 1, heads, d), dtype)
+    assert bytes_of(kvc, q) > 0 and bytes_of(kvc, q, 1025) > 0 and bytes_of(kvc, q, 1024) == 0
+    for bound in (0, 2050, 1025, 1024, 1):
+        out = sense.sense_kv_attention(kvc, 0, q, max_kv=bound)
+        compare(out, q, m, 0, range(6), [1] * 6)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("d,heads,kv,nodes", [(128, 8, 2, 61), (64, 4, 1, 75), (64, 6, 2, 50),
+                                              (256, 4, 1, 30), (128, 4, 1, 16), (128, 2, 1, 9),
+                                              (64, 8, 2, 130)])
+def test_trees_behind_long_contexts(dtype, d, heads, kv, nodes):
+    """Masked trees in tiles of 128, 64, 32 and 16 rows, cut into runs; rows
+    that see nothing but the prefix, and one that sees nothing at all."""
+    print(f"[kv runs] tree {dtype} d={d} {heads}/{kv} nodes={nodes}", flush=True)
+    rng = np.random.default_rng(nodes + d)
+    counts = [nodes, nodes // 2, nodes]
+    lens = [1400 + nodes, 2100, nodes]
+    kvc, m = pair(rng, lens, page=32, heads=kv, d=d)
+    masks = (rng.random((3, nodes, nodes)) < 0.3).astype(np.uint8)
+    masks[0, 1] = 0
+    masks[2, nodes - 1] = 0
+    q = queries(rng, (3, nodes, heads, d), dtype)
+    gmask = torch.tensor(masks, device=DEV)
+    assert bytes_of(kvc, q) > 0 and bytes_of(kvc, q, 1024) == 0
+    for bound in (0, 1024):
+        out = sense.sense_kv_attention(kvc, 0, q, mask=gmask, row_len=ints(counts), max_kv=bound,
+                                       out=torch.full_like(q, 4))
+        compare(out, q, m, 0, range(3), counts, masks=masks)
+        assert (out[2, nodes - 1] == 0).all() and (out[1, counts[1]:] == 4).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("d,heads,kv,rows", [(64, 4, 1, 75), (64, 2, 2, 300), (128, 4, 2, 75),
+                                             (256, 2, 1, 75)])
+def test_chunks_behind_long_contexts(dtype, d, heads, kv, rows):
+    """Causal chunks of several tiles of rows, cut; beside single tokens."""
+    print(f"[kv runs] chunk {dtype} d={d} {heads}/{kv} rows={rows}", flush=True)
+    rng = np.random.default_rng(rows + d)
+    lens, counts = [1300 + rows, 40, 2000, rows], [rows, 1, 1, rows]
+    kvc, m = pair(rng, lens, page=64, heads=kv, d=d)
+    q = queries(rng, (4, rows, heads, d), dtype)
+    assert bytes_of(kvc, q) > 0
+    out = sense.sense_kv_attention(kvc, 0, q, row_len=ints(counts))
+    compare(out, q, m, 0, range(4), counts)
+
+
+@pytest.mark.parametrize("d,rows", [(64, 30), (128, 1), (128, 25)])
+def test_more_than_64_entries_of_each_kind(d, rows):
+    """One call of tokens, trees and chunks, most of them short, two long."""
+    print(f"[kv runs] mixed d={d} rows={rows}", flush=True)
+    rng = np.random.default_rng(rows + d)
+    n, heads = 80, 6
+    counts = rng.integers(0, rows + 1, n)
+    counts[[7, 64, 79]] = rows
+    lens = counts + rng.integers(0, 90, n)
+    lens[7] += 1800
+    lens[64] += 1100
+    kvc, m = pair(rng, lens.tolist(), page=16, heads=2, d=d)
+    q = queries(rng, (n, rows, heads, d), "bf16")
+    assert bytes_of(kvc, q) > 2 * bytes_of(kvc, q, 1024)
+    out = sense.sense_kv_attention(kvc, 0, q, row_len=ints(counts), out=torch.full_like(q, 6))
+    for i in (0, 1, 7, 8, 63, 64, 65, 79):
+        compare(out[i:i + 1], q[i:i + 1], m, 0, [i], [int(counts[i])])
+        assert (out[i, counts[i]:] == 6).all()
