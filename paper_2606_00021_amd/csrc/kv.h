@@ -69,6 +69,28 @@ __device__ __forceinline__ int kv_rows(const KvBatch& b, int i) {
 __device__ __forceinline__ int64_t kv_start(const KvBatch& b, int i) {
     return b.row_start ? (int64_t)b.row_start[i] : (int64_t)i * b.max_rows;
 }
+
+// Inclusive prefix sums over the threads of a workgroup that plans alone, in
+// their order; s_wave is its scratch, a number a wave.
+constexpr int kPlanThreads = 1024;
+__device__ __forceinline__ int64_t block_scan(int64_t v, int64_t* s_wave, int64_t* total) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+    for (int s = 1; s < 64; s <<= 1) {
+        const int64_t o = __shfl_up((long long)v, s);
+        if (lane >= s) v += o;
+    }
+    if (lane == 63) s_wave[wave] = v;
+    __syncthreads();
+    int64_t before = 0, all = 0;
+    for (int w = 0; w < kPlanThreads / 64; ++w) {
+        if (w < wave) before += s_wave[w];
+        all += s_wave[w];
+    }
+    __syncthreads();
+    *total = all;
+    return v + before;
+}
 #endif
 
 // Rows of n_layers layers from `layer` on; strides in elements, head h of a
@@ -106,9 +128,6 @@ size_t kv_attention_workspace_bytes(int n, int max_rows, int n_heads, int kv_hea
                                     int max_kv);
 hipError_t launch_kv_attention(const KvCache& c, const KvBatch& b, const KvAttention& a,
                                void* workspace, hipStream_t st);
-
-// The message of sense_last_error_message() on this thread (sense_api.hip).
-void set_last_error(const char* msg);
 
 // Page operations (kv_pages.hip); status may be NULL.
 size_t kv_reserve_workspace_bytes(int n, int n_pages);

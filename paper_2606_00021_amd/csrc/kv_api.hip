@@ -1,11 +1,8 @@
 // Host layer of the 4-bit paged key/value cache (the sense_kv_* entry points
 // of include/sense.h): argument validation, workspace sizes, launches.
-#include <math.h>
-#include <stdarg.h>
-#include <stdio.h>
-
 #include <initializer_list>
 
+#include "host.h"
 #include "internal.h"
 #include "kv.h"
 #include "sense.h"
@@ -14,30 +11,16 @@
 
 namespace {
 
+using sense::aligned;
+using sense::fail;
 using sense::KvBatch;
 using sense::KvCache;
-
-sense_status_t fail(sense_status_t st, const char* fmt, ...) {
-    char msg[512];
-    va_list ap;
-    va_start(ap, fmt);
-    vsnprintf(msg, sizeof msg, fmt, ap);
-    va_end(ap);
-    sense::set_last_error(msg);
-    return st;
-}
-
-sense_status_t ok() {
-    sense::set_last_error("");
-    return SENSE_OK;
-}
+using sense::ok;
 
 sense_status_t launched(hipError_t e, const char* where) {
     if (e == hipSuccess) return ok();
     return fail(SENSE_ERR_HIP, "%s: %s", where, hipGetErrorString(e));
 }
-
-bool aligned(const void* p, size_t a) { return ((uintptr_t)p % a) == 0; }
 
 // One dispatch holds fewer than 2^32 work-items per dimension; workgroups here
 // have up to 256.

@@ -186,26 +186,6 @@ __device__ __forceinline__ Plan plan_few(const Args& g) {
 }
 
 // The same for more entries, by one workgroup in front of the attention.
-constexpr int kPlanThreads = 1024;
-__device__ __forceinline__ int64_t block_scan(int64_t v, int64_t* s_wave, int64_t* total) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll
-    for (int s = 1; s < 64; s <<= 1) {
-        const int64_t o = __shfl_up((long long)v, s);
-        if (lane >= s) v += o;
-    }
-    if (lane == 63) s_wave[wave] = v;
-    __syncthreads();
-    int64_t before = 0, all = 0;
-    for (int w = 0; w < kPlanThreads / 64; ++w) {
-        if (w < wave) before += s_wave[w];
-        all += s_wave[w];
-    }
-    __syncthreads();
-    *total = all;
-    return v + before;
-}
-
 template <int ROWS>
 __global__ __launch_bounds__(kPlanThreads) void kv_plan_kernel(Args g) {
     __shared__ int64_t s_wave[kPlanThreads / 64];
@@ -465,7 +445,6 @@ __global__ __launch_bounds__(kThreads, MT * D > 128 || MT == 2 ? 2 : (D == 128 ?
     const int col = lane & 15, grp = lane >> 4;
     const int local = item - p.first;
     const int split = local / g.c.heads, head = local - split * g.c.heads;
-    constexpr int r0 = 0;                       // a unit is one tile
     const int base = p.len - p.rows;            // position of the first new token
     const int64_t start = kv_start(g.b, p.entry);
 
@@ -474,7 +453,7 @@ __global__ __launch_bounds__(kThreads, MT * D > 128 || MT == 2 ? 2 : (D == 128 ?
     u32x4 qf[MT][kKs];
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
-        const int r = r0 + mt * 16 + col;
+        const int r = mt * 16 + col;
         tok[mt] = r / g.group;
         const int64_t row = start + tok[mt];
         const bool on = tok[mt] < p.rows && row >= 0 && row < g.b.n_rows;
@@ -491,10 +470,10 @@ __global__ __launch_bounds__(kThreads, MT * D > 128 || MT == 2 ? 2 : (D == 128 ?
     if (key1 > p.len) key1 = p.len;
     int full = base;
     if (!g.a.mask) {
-        const int last = (r0 + kRows - 1) / g.group;
+        const int last = (kRows - 1) / g.group;
         const int seen = base + (last < p.rows ? last : p.rows - 1) + 1;
         if (key1 > seen) key1 = seen;
-        full = base + r0 / g.group + 1;
+        full = base + 1;
     }
 
     f32x4 o[DV][MT];
@@ -752,7 +731,7 @@ __global__ __launch_bounds__(kThreads, MT * D > 128 || MT == 2 ? 2 : (D == 128 ?
     __syncthreads();
     for (int at = threadIdx.x; at < kRows * (D / 4); at += kThreads) {
         const int r = at / (D / 4), dim = at % (D / 4) * 4;
-        const int rr = r0 + r, token = rr / g.group;
+        const int token = r / g.group;
         const int64_t row = start + token;
         if (token >= p.rows || row < 0 || row >= g.b.n_rows) continue;
         float top = s_m[0][r];
@@ -770,7 +749,7 @@ __global__ __launch_bounds__(kThreads, MT * D > 128 || MT == 2 ? 2 : (D == 128 ?
             // Nothing seen: 0.  A sum of NaN is not 0.
             const float inv = l == 0.f ? 0.f : 1.f / l;
             uint32_t* dst = (uint32_t*)((uint16_t*)g.a.out + row * g.a.out_stride +
-                                        ((int64_t)head * g.group + rr % g.group) * D + dim);
+                                        ((int64_t)head * g.group + r % g.group) * D + dim);
             dst[0] = pack<F16>(sum[0] * inv, sum[1] * inv);
             dst[1] = pack<F16>(sum[2] * inv, sum[3] * inv);
         } else {

@@ -18,7 +18,6 @@
 namespace sense {
 namespace {
 
-constexpr int kPlanThreads = 1024;
 constexpr int kThreads = 256;
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
@@ -102,26 +101,6 @@ __global__ __launch_bounds__(kThreads) void kv_fork_kernel(KvCache c, const int3
 
 // ------------------------------------------------------------------- grow
 
-// Inclusive prefix sums over the workgroup's threads.
-__device__ __forceinline__ int64_t block_scan(int64_t v, int64_t* s_wave, int64_t* total) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll
-    for (int s = 1; s < 64; s <<= 1) {
-        const int64_t o = __shfl_up((long long)v, s);
-        if (lane >= s) v += o;
-    }
-    if (lane == 63) s_wave[wave] = v;
-    __syncthreads();
-    int64_t before = 0, all = 0;
-    for (int w = 0; w < kPlanThreads / 64; ++w) {
-        if (w < wave) before += s_wave[w];
-        all += s_wave[w];
-    }
-    __syncthreads();
-    *total = all;
-    return v + before;
-}
-
 // A page to be copied: the filled slots of `src` to `dst`, in every layer.
 struct Copy {
     int32_t src, dst, fill;
@@ -174,11 +153,7 @@ __global__ __launch_bounds__(kPlanThreads) void kv_reserve_kernel(KvCache c, con
     for (int i = tid; i < n; i += kPlanThreads) {
         const int last = s_last[i];
         if (last < 0 || s_need[i] < 0) continue;
-        const int refs = c.page_refs[last];
-        if (refs <= 1) {
-            s_last[i] = -1 - last;                   // nobody else: not copied
-            continue;
-        }
+        if (c.page_refs[last] <= 1) s_last[i] = -1 - last;   // nobody else: not copied
     }
     __syncthreads();
     int mine[kKvMaxEntries / kPlanThreads];

@@ -11,8 +11,8 @@
 #include <mutex>
 #include <new>
 
+#include "host.h"
 #include "internal.h"
-#include "kv.h"
 #include "sense.h"
 
 #define SENSE_EXPORT extern "C" __attribute__((visibility("default")))
@@ -50,9 +50,26 @@ struct sense_index {
     int64_t* cap_prefix;     // host: sums of the p largest list sizes, p = 0..nlist
 };
 
+static thread_local char g_msg[512];
+
+sense_status_t sense::fail(sense_status_t st, const char* fmt, ...) {
+    va_list ap;
+    va_start(ap, fmt);
+    vsnprintf(g_msg, sizeof g_msg, fmt, ap);
+    va_end(ap);
+    return st;
+}
+
+sense_status_t sense::ok() {
+    g_msg[0] = '\0';
+    return SENSE_OK;
+}
+
 namespace {
 
-thread_local char g_msg[512];
+using sense::aligned;
+using sense::fail;
+using sense::ok;
 
 // Timing events per sense_timer_t, set by sense_set_timer_events.
 constexpr int kTimers = 8;
@@ -63,24 +80,9 @@ hipError_t timer_mark(int which, int edge, hipStream_t st) {
     return ev ? hipEventRecord(ev, st) : hipSuccess;
 }
 
-sense_status_t fail(sense_status_t st, const char* fmt, ...) {
-    va_list ap;
-    va_start(ap, fmt);
-    vsnprintf(g_msg, sizeof g_msg, fmt, ap);
-    va_end(ap);
-    return st;
-}
-
-sense_status_t ok() {
-    g_msg[0] = '\0';
-    return SENSE_OK;
-}
-
 sense_status_t hip_fail(hipError_t e, const char* where) {
     return fail(SENSE_ERR_HIP, "%s: %s", where, hipGetErrorString(e));
 }
-
-bool aligned(const void* p, size_t a) { return ((uintptr_t)p % a) == 0; }
 
 size_t round_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
@@ -206,8 +208,6 @@ SENSE_EXPORT const char* sense_status_string(sense_status_t s) {
     }
     return "unknown status";
 }
-
-void sense::set_last_error(const char* msg) { snprintf(g_msg, sizeof g_msg, "%s", msg); }
 
 SENSE_EXPORT const char* sense_last_error_message(void) { return g_msg; }
 
