@@ -759,6 +759,8 @@ sense_status_t sense_kv_attention_workspace_size(const sense_kv_cache_t *cache, 
  * n_heads / n_kv_heads), whatever the batch holds beside them, and 11 bits in
  * larger ones.  NaN that a row sees makes it NaN: a key's the whole row, a
  * value's the dims of its block.
+ * Sums are those of weights up to 2^15 times values before they are divided by
+ * the weights' sum: values that a row sees of 2^80 or more may overflow it.
  *   q, out      rows of n_heads x head_dim elements of q_dtype (F16, BF16),
  *               head h at h * head_dim; strides in elements; bases and strides
  *               multiples of 16 bytes.  out may be q.  Rows that the batch

@@ -171,3 +171,34 @@ def test_values_of_any_size(d, rows, heads):
                        + (n + 8) * 2.0 ** -23 * big
                        + n * 2.0 ** -30 * np.abs(v[:end]).max(0) + 2.0 ** -120)
                 assert (np.abs(out[i, j, h] - o) <= tol).all(), (i, j, h)
+
+
+@pytest.mark.parametrize("d,rows,heads", [(64, 1, 4), (128, 4, 4), (128, 3, 16), (128, 4, 40),
+                                          (256, 5, 16)])
+def test_values_just_below_2_to_the_80(d, rows, heads):
+    """bf16, over long sequences: sums of weights times values stay finite.
+    Bound as above."""
+    print(f"[kv weights] huge values d={d} rows={rows}x{heads}", flush=True)
+    rng = np.random.default_rng(d + heads)
+    lens = [1300, 40]
+    kvc, m = pair(rng, lens, page=64, heads=1, d=d)
+    m.scales[:, :, 1] = 127 + 77
+    m.codes[:, :, 1] = rng.choice([0x66, 0x77, 0x75], m.codes[:, :, 1].shape)   # 4 and 6, 3
+    kvc = up(m)
+    q = torch.tensor(rng.standard_normal((2, rows, heads, d))).to(torch.bfloat16).to(DEV)
+    for bound in (0, 1024):
+        out = sense.sense_kv_attention(kvc, 0, q, max_kv=bound).double().cpu().numpy()
+        for i, n in enumerate(lens):
+            k, v = m.rows(0, i, 0, n)[:, :, 0]
+            for j in range(rows):
+                end = n - rows + j + 1
+                s = k[:end] @ q[i, j].double().cpu().numpy().T * d ** -0.5     # [end, heads]
+                p = np.exp(s - s.max(0))
+                p /= p.sum(0)
+                o = p.T @ v[:end]
+                size = np.abs(k[:end]) @ np.abs(q[i, j].double().cpu().numpy()).T * d ** -0.5
+                ds = ((d + 4) * 2.0 ** -23 * size.max(0) + 2.0 ** -21)[:, None]
+                spread = np.stack([p[:, h] @ np.abs(v[:end] - o[h]) for h in range(heads)])
+                tol = (2.0 ** -8 * np.abs(o) + (2.0 ** -11 + 2 * ds) * spread
+                       + ((n + 8) * 2.0 ** -23 + n * 2.0 ** -30) * np.abs(v).max())
+                assert (np.abs(out[i, j] - o) <= tol).all(), (i, j)
