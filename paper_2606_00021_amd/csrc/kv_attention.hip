@@ -87,9 +87,9 @@ struct Args {
     KvAttention a;
     int group;          // query heads per key head
     int target;         // workgroups that the work is cut for (0: units stay whole)
-    float* part_o;      // [item][rows][d]
-    f32x2* part_ml;     // [item][rows]: reference (a score), sum
-    i32x4* plans;       // [entry]: new tokens, first item, runs of a unit, tiles of a run
+    float* part_o;      // [item of a cut unit][rows][d]
+    f32x2* part_ml;     // [the same][rows]: reference (a score), sum
+    i32x4* plans;       // [entry]: new tokens, first item, runs of a unit, first cut item
 };
 
 // Where one unit tile's items lie, and which keys one of them has.
@@ -98,6 +98,7 @@ struct Plan {
     int entry, seq;     // entry of the item (-1: none)
     int rows, len;      // new tokens of the entry, cached positions
     int first;          // first item of the entry
+    int part;           // the item's place among those of cut units
     int splits;         // runs of a unit of the entry
     int run;            // tiles of kTile keys in a run
 };
@@ -166,8 +167,10 @@ __device__ __forceinline__ Plan plan_few(const Args& g) {
         const int longer = (int)divide((int64_t)run * total, g.target);
         run = __builtin_amdgcn_readfirstlane(longer > run ? longer : run + 1);
     }
+    const int cut = splits_of(z0.tiles, run) > 1 ? mine : 0, cut_first = wave_scan(cut) - cut;
     if (g.target && blockIdx.x == 0 && threadIdx.x < g.b.n)
-        g.plans[threadIdx.x] = i32x4{z0.rows, upto - mine, splits_of(z0.tiles, run), run};
+        g.plans[threadIdx.x] =
+            i32x4{z0.rows, upto - mine, splits_of(z0.tiles, run), cut_first};
     Plan p;
     p.item = (int)blockIdx.x;
     p.entry = -1;
@@ -179,6 +182,7 @@ __device__ __forceinline__ Plan plan_few(const Args& g) {
     p.rows = __builtin_amdgcn_readlane(z0.rows, src);
     p.len = __builtin_amdgcn_readlane(z0.len, src);
     p.first = __builtin_amdgcn_readlane(upto - mine, src);
+    p.part = __builtin_amdgcn_readlane(cut_first, src) + p.item - p.first;
     p.run = run;
     p.splits = __builtin_amdgcn_readfirstlane(
         splits_of(__builtin_amdgcn_readlane(z0.tiles, src), run));
@@ -213,16 +217,18 @@ __global__ __launch_bounds__(kPlanThreads) void kv_plan_kernel(Args g) {
         const int longer = (int)divide((int64_t)run * total, g.target);
         run = longer > run ? longer : run + 1;
     }
+    // Items, and in the high half those of cut units: fewer than 2^25 of either.
     int64_t at = 0;
     for (int e0 = 0; e0 < g.b.n; e0 += kPlanThreads) {
         const int e = e0 + threadIdx.x;
         Size z = {-1, 0, 0, 0, 0};
         if (e < g.b.n) z = size_of<ROWS>(g, e);
         const int splits = splits_of(z.tiles, run);
-        const int64_t mine = (int64_t)z.units * splits * g.c.heads;
+        const int64_t items = (int64_t)z.units * splits * g.c.heads;
+        const int64_t mine = items + (splits > 1 ? items << 32 : 0);
         int64_t total;
-        const int64_t upto = block_scan(mine, s_wave, &total);
-        if (e < g.b.n) g.plans[e] = i32x4{z.rows, (int)(at + upto - mine), splits, run};
+        const int64_t first = at + block_scan(mine, s_wave, &total) - mine;
+        if (e < g.b.n) g.plans[e] = i32x4{z.rows, (int)first, splits, (int)(first >> 32)};
         at += total;
     }
     if (threadIdx.x == 0) g.plans[g.b.n] = i32x4{0, (int)at, 1, run};
@@ -255,7 +261,8 @@ __device__ __forceinline__ Plan plan_many(const Args& g) {
     const i32x4 x = g.plans[from];
     p.first = __builtin_amdgcn_readfirstlane(x[1]);
     p.splits = __builtin_amdgcn_readfirstlane(x[2]);
-    p.run = __builtin_amdgcn_readfirstlane(x[3]);
+    p.part = __builtin_amdgcn_readfirstlane(x[3]) + p.item - p.first;
+    p.run = __builtin_amdgcn_readfirstlane(g.plans[g.b.n][3]);
     return p;
 }
 
@@ -438,12 +445,11 @@ __global__ __launch_bounds__(kThreads, MT * D > 128 || MT == 2 ? 2 : (D == 128 ?
 
     const Plan p = plan<kRows>(g);
     if (p.entry < 0) return;
-    const int item = p.item;
 
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 15, grp = lane >> 4;
-    const int local = item - p.first;
+    const int local = p.item - p.first;
     const int split = local / g.c.heads, head = local - split * g.c.heads;
     const int base = p.len - p.rows;            // position of the first new token
     const int64_t start = kv_start(g.b, p.entry);
@@ -753,8 +759,8 @@ __global__ __launch_bounds__(kThreads, MT * D > 128 || MT == 2 ? 2 : (D == 128 ?
             dst[0] = pack<F16>(sum[0] * inv, sum[1] * inv);
             dst[1] = pack<F16>(sum[2] * inv, sum[3] * inv);
         } else {
-            *(f32x4*)(g.part_o + ((int64_t)item * kRows + r) * D + dim) = sum;
-            if (dim == 0) g.part_ml[(int64_t)item * kRows + r] = f32x2{top, l};
+            *(f32x4*)(g.part_o + ((int64_t)p.part * kRows + r) * D + dim) = sum;
+            if (dim == 0) g.part_ml[(int64_t)p.part * kRows + r] = f32x2{top, l};
         }
     }
 }
@@ -1199,7 +1205,7 @@ __global__ __launch_bounds__(kThreads, D >= 128 ? 2 : (MT == 1 ? 4 : 3))
                 dst[at / 8] = x;
             }
         } else {
-            float* dst = g.part_o + ((int64_t)p.item * kRows + r) * D + 4 * DV * grp;
+            float* dst = g.part_o + ((int64_t)p.part * kRows + r) * D + 4 * DV * grp;
             const float less = __builtin_amdgcn_exp2f(-surplus(ref[mt], cs, kLift));
 #pragma unroll
             for (int at = 0; at < 4 * DV; at += 4) {
@@ -1208,7 +1214,7 @@ __global__ __launch_bounds__(kThreads, D >= 128 ? 2 : (MT == 1 ? 4 : 3))
                     f32x4{o[t][mt][q], o[t + 1][mt][q], o[t + 2][mt][q], o[t + 3][mt][q]} * less +
                     (hit[mt][q] > 0.f ? NAN : 0.f);
             }
-            if (grp == 0) g.part_ml[(int64_t)p.item * kRows + r] = f32x2{ref[mt], l * less};
+            if (grp == 0) g.part_ml[(int64_t)p.part * kRows + r] = f32x2{ref[mt], l * less};
         }
     }
 }
@@ -1227,7 +1233,7 @@ __global__ __launch_bounds__(kThreads) void kv_join_kernel(Args g, int tiles_max
     const int head = blockIdx.x / per_tile / tiles_max % g.c.heads;
     const int entry = blockIdx.x / per_tile / tiles_max / g.c.heads;
     const i32x4 plan = g.plans[entry];
-    const int rows = plan[0], first_item = plan[1], splits = plan[2];
+    const int rows = plan[0], splits = plan[2], first_part = plan[3];
     if (splits == 1) return;
     const int n_tiles = (rows * g.group + ROWS - 1) / ROWS;
     if (rt >= n_tiles) return;
@@ -1246,7 +1252,7 @@ __global__ __launch_bounds__(kThreads) void kv_join_kernel(Args g, int tiles_max
             // The partial sums come from far (other XCDs wrote them): many at
             // a time; places behind the last read the first again, weight 0.
             constexpr int kEvery = RB == 1 ? kTeams : 1;
-            const int64_t first = ((int64_t)first_item + place) * ROWS + r;
+            const int64_t first = ((int64_t)first_part + place) * ROWS + r;
             const int64_t apart = (int64_t)g.c.heads * n_tiles * ROWS;
             auto add = [&](auto batch) {
                 constexpr int kBatch = decltype(batch)::value;
@@ -1313,8 +1319,11 @@ __global__ __launch_bounds__(kThreads) void kv_join_kernel(Args g, int tiles_max
 // of 128: two 2048-token chunks over 6000 positions 356 us, 497 in tiles of 64.
 // Tiles of 64 where the unit has no more, of 256 dims, whose sums take twice
 // the registers, and of 64 dims where they leave a quarter of the rows less
-// empty (183 rows, 16 entries over 200 to 4100 positions: 36.1 us, 39.6 in
-// tiles of 128; all over 2000: 45.7, 45.0; 300 rows, not a quarter: 55.8, 51.8).
+// empty, which is from 129 to 192 rows.  Tiles of 64 and 128 there, us: 16 entries
+// over 200 to 4100 positions of 129, 183, 192 rows 32.7, 35.0, 34.7 and 38.9,
+// 40.6, 39.3; 1 of 183 over 8000 24.2 and 26.9; 32 over 1500 50.8 and 56.9; 8 of
+// 140 over 1000 26.5 and 34.6; 16 of 188 over 4000 73 and 63.  And where it is
+// not a quarter: 65 rows 31.9 and 29.7, 210 44.8 and 40.7, 300 51.8 and 49.8.
 int tile_rows(int max_rows, int group, int d) {
     const int64_t rows = (int64_t)max_rows * group;
     if (rows <= 16) return 16;
@@ -1326,9 +1335,11 @@ int tile_rows(int max_rows, int group, int d) {
 
 // Workgroups to cut the work for: what is resident at once (twice and three
 // times as many took 41 -> 46, 48 us for one token over 131K positions: each
-// costs its start and a partial sum; the four that 64-row tiles of 64 dims
-// leave room for against three: 183 rows, 16 entries of 200 to 4100 positions
-// 40.1 -> 36.0 us, all of 2000 45.0 -> 45.4).
+// costs its start and a partial sum).  Tiles of 64 rows of 64 dims leave room for
+// four on a compute unit; four against three, us: 16 entries over 200 to 4100
+// positions of 129, 183, 192 rows 32.7, 35.0, 34.7 and 36.5, 38.7, 38.6; 32 of 183
+// over 1500 50.8 and 50.3; 2 of 150 over 300 and 9000 29.7 and 27.1; 16 of 188
+// over 4000 each, where the last few have the device to themselves, 73 and 63.
 int target_items(int rows, int d) {
     if (rows > 32) return device_cus() * (d >= 128 ? 2 : (rows == 64 ? 4 : 3));
     return device_cus() * (rows > 16 || d == 256 ? 2 : (d == 128 ? 3 : 4));
@@ -1382,7 +1393,11 @@ int64_t kv_attention_blocks(int n, int max_rows, int n_heads, int kv_heads, int 
     return units * (rows == 16 ? 16 : rows / 16) + target_items(rows, d);
 }
 
-// Partial sums, where units may be cut, and the entries' plans.
+// Partial sums of the items of cut units, and the entries' plans.  There are at
+// most `target` more items than units, and at most 2 target of cut units: a run
+// has at least (tiles of all units) / target tiles and a cut unit more than one
+// run, so all cut units' tiles are at most target runs, and there are fewer cut
+// units than that; each unit's last run may be a part of one.
 struct Layout {
     int rows, target;
     size_t ml, plans, total;
@@ -1391,9 +1406,10 @@ Layout layout_of(int n, int max_rows, int n_heads, int kv_heads, int d, int max_
     Layout l;
     l.rows = tile_rows(max_rows, n_heads / kv_heads, d);
     l.target = max_kv > kWhole ? target_items(l.rows, d) : 0;
+    const int64_t units = units_most(n, max_rows, n_heads, kv_heads, l.rows);
     const size_t rows =
-        l.target ? (size_t)(units_most(n, max_rows, n_heads, kv_heads, l.rows) + l.target) * l.rows
-                 : 0;
+        (size_t)(units < l.target ? units + l.target : 2 * (int64_t)l.target) * l.rows *
+        (l.target != 0);
     l.ml = align256(rows * d * sizeof(float));
     l.plans = l.ml + align256(rows * sizeof(f32x2));
     l.total = l.plans + (l.target || n > 64 ? align256((size_t)(n + 1) * sizeof(i32x4)) : 0);

@@ -8,7 +8,7 @@ import torch
 
 from kv_gpu import DEV, ints, pair
 from paper_2606_00021_amd import sense
-from test_gpu_kv_attention import compare, queries
+from test_gpu_kv_attention import compare, queries, reference, sees
 
 pytestmark = pytest.mark.gpu
 
@@ -125,3 +125,50 @@ def test_more_than_64_entries_of_each_kind(d, rows):
     for i in (0, 1, 7, 8, 63, 64, 65, 79):
         compare(out[i:i + 1], q[i:i + 1], m, 0, [i], [int(counts[i])])
         assert (out[i, counts[i]:] == 6).all()
+
+
+@pytest.mark.parametrize("d,n,heads,long", [(64, 64, 16, 59), (128, 70, 12, 60)])
+def test_as_many_partial_sums_as_there_can_be(d, n, heads, long):
+    """Almost as many units as workgroups, nearly all a little longer than a run:
+    each is cut in two, and the units alone fill the device, so that the plan does
+    not look for longer runs.  Nothing behind the workspace is touched."""
+    print(f"[kv runs] most partial sums d={d} n={n}", flush=True)
+    rng = np.random.default_rng(d)
+    lens = [2048] * long + [3] * (n - long)
+    kvc, m = pair(rng, lens, page=128, heads=heads, d=d)
+    q = queries(rng, (n, 1, heads, d), "bf16")
+    size = bytes_of(kvc, q)
+    room = torch.full((size + (1 << 22),), 171, dtype=torch.uint8, device=DEV)
+    out = sense.sense_kv_attention(kvc, 0, q, workspace=room[:size])
+    assert (room[size:] == 171).all()
+    for i in (0, long // 2, long - 1, long, n - 1):
+        compare(out[i:i + 1], q[i:i + 1], m, 0, [i], [1])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("d,heads", [(64, 8), (128, 4), (256, 4)])
+def test_tokens_beside_a_long_chunk(dtype, d, heads):
+    """One chunk of 300 rows among tokens, some of long and some of no context."""
+    print(f"[kv runs] beside a chunk {dtype} d={d}", flush=True)
+    rng = np.random.default_rng(d + heads)
+    for n in (20, 66):
+        counts = [1] * n
+        counts[5] = 300
+        lens = rng.integers(0, 100, n)
+        lens[[0, 5, 11, n - 1]] = 1800, 1500, 1300, 2600
+        kvc, m = pair(rng, lens.tolist(), page=64, heads=2, d=d)
+        q = queries(rng, (n, 300, heads, d), dtype)
+        size = bytes_of(kvc, q)
+        room = torch.full((size + (1 << 22),), 171, dtype=torch.uint8, device=DEV)
+        out = sense.sense_kv_attention(kvc, 0, q, row_len=ints(counts), workspace=room[:size],
+                                       out=torch.full_like(q, 2))
+        assert (room[size:] == 171).all()
+        at = [0, 1, 2, 11, n - 1]
+        for i in at:
+            if lens[i]:
+                compare(out[i:i + 1], q[i:i + 1], m, 0, [i], [1])
+            assert (out[i, 1:] == 2).all()
+        pick = [0, 1, 150, 299]
+        o = out[5:6][:, pick]
+        ref, tol = reference(q[5, pick], m.rows(0, 5, 0, 1500), d ** -0.5, sees(300, 1500)[pick])
+        assert ((o[0].double().cpu() - ref).abs() <= tol).all()
