@@ -751,16 +751,17 @@ sense_status_t sense_kv_attention_workspace_size(const sense_kv_cache_t *cache, 
  *               mask[i * mask_stride + j * mask_ld + u] != 0
  * (for a draft tree the mask of sense_build_loose_trie, row_len its tree_len).
  * A row whose own position base + j is below 0 sees nothing, whatever its mask
- * names.  A row that sees nothing becomes 0.  Positions that a row does not see do not
- * touch it, whatever they hold.  Statistics and sums are fp32; cached values
- * are exact for BF16 queries (all that sense_kv_write writes); for F16 ones F16
- * has to hold them: a row that sees a block of a scale above 2^13 is unspecified.
- * Weights carry at least 16 bits in entries of up to 64 rows (row_len times
- * n_heads / n_kv_heads), whatever the batch holds beside them, and 11 bits in
- * larger ones.  NaN that a row sees makes it NaN: a key's the whole row, a
- * value's the dims of its block.
- * Sums are those of weights up to 2^15 times values before they are divided by
- * the weights' sum: values that a row sees of 2^80 or more may overflow it.
+ * names.  A row that sees nothing becomes 0.  Positions that a row does not see
+ * do not touch it, whatever they hold.  NaN that a row sees makes it NaN: a key's
+ * the whole row, a value's the dims of its block.
+ * Statistics and sums are fp32.  Cached values are exact for BF16 queries (all
+ * that sense_kv_write writes); for F16 ones F16 has to hold them: a row that sees
+ * a block of a scale above 2^13 is unspecified.  Weights carry at least 16 bits
+ * in entries of up to 64 rows (row_len times n_heads / n_kv_heads), whatever the
+ * batch holds beside them, and 11 bits in larger ones, but no finer than steps of
+ * 2^-31 of a row's largest.  Sums are those of weights up to 2^15 times values,
+ * before the division by the weights' sum: values that a row sees of 2^80 or more
+ * may overflow them.
  *   q, out      rows of n_heads x head_dim elements of q_dtype (F16, BF16),
  *               head h at h * head_dim; strides in elements; bases and strides
  *               multiples of 16 bytes.  out may be q.  Rows that the batch

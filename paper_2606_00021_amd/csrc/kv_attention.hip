@@ -18,10 +18,11 @@
 // (kv_many_kernel).
 //
 // Few rows are bound by the bytes of the cache: 64 streams of 8000 positions
-// (32 / 8 heads of 128, 557 MB) take 111 us, 5.0 TB/s, where a plain read of as
-// many bytes takes 80.  Many rows are bound by the matrix and vector units
-// (exponentials): two 2048-token chunks over 6000 positions 356 us, 937
-// TFLOP/s, where a large bf16 product of the library reaches 1170.
+// (32 / 8 heads of 128, 558 MB) take 97 to 103 us, 5.4 to 5.8 TB/s, where a plain
+// read of as many bytes takes 78 to 80.  Many rows are bound by the matrix and
+// vector units (exponentials): two 2048-token chunks, of 2048 and 10000
+// positions, 341 us, 984 TFLOP/s, where a large bf16 product of the library
+// reaches 1170.
 //
 // Both products run on the matrix cores, transposed:
 //   S^T = K Q^T   A = K (16 keys x 32 dims), B = Q^T (32 dims x 16 rows)
@@ -768,7 +769,8 @@ __global__ __launch_bounds__(kThreads, MT * D > 128 || MT == 2 ? 2 : (D == 128 ?
 // The same for many rows (draft trees, prompt chunks): a workgroup's four
 // waves have 16 MT rows each and share the keys.  A tile of KT keys is widened
 // once for all of them and laid into LDS in the order in which the matrix
-// instructions take it (fragments of 16 bytes a lane: no conflicts), two tiles
+// instructions take it, in fragments of 16 bytes a lane (bank conflicts are 14 % of
+// the LDS's cycles, in which it is busy a third of the time), two tiles
 // in turn, so that one is read while the next is written; a wave widens 16
 // keys (or their keys or values alone).  Each wave ends with whole rows, so
 // nothing is joined but runs.
@@ -776,7 +778,7 @@ __global__ __launch_bounds__(kThreads, MT * D > 128 || MT == 2 ? 2 : (D == 128 ?
 // Keys are widened to the query's type, values to f16.  A part with a scale
 // outside 2^-19 .. 2^12 (one test of four bytes) is looked at value by value: what
 // f16 does not hold is 0 in LDS, and each wave fetches it again in bf16, for
-// products of its own.  Two 2048-token chunks take 339 us, as with weights and
+// products of its own.  Two 2048-token chunks take 341 us, as with weights and
 // values in bf16 (344; with values of both kinds in LDS and a mask: 391).  Where
 // every value is beyond f16 they take 2.8 times as long.
 template <int D, bool F16, int MT>
@@ -841,8 +843,9 @@ __global__ __launch_bounds__(kThreads, D >= 128 ? 2 : (MT == 1 ? 4 : 3))
     }
     if (w0 / g.group >= p.rows) end = 0;        // no rows: the wave only widens
     // Weights as two numbers where the entry has no more rows than this, whatever
-    // lies beside it: 48 rows over 200 to 4100 positions 26.1 -> 28.3 us; 183 rows
-    // would pay 35.0 -> 39.5, two 2048-token chunks 352 -> 446.
+    // lies beside it: 48 rows of 128 dims over 200 to 4100 positions 25.8 -> 28.4
+    // us; 183 rows of 64 would pay 33.8 -> 38.1, 1204 of 128 over 8500 positions
+    // 75 -> 91, two 2048-token chunks 337 -> 444.
     const bool two = p.rows * g.group <= 64;
 
     f32x4 o[DV][MT];
@@ -1316,7 +1319,7 @@ __global__ __launch_bounds__(kThreads) void kv_join_kernel(Args g, int tiles_max
 // Rows of a tile.  Up to 32 rows of a unit are one tile of the kernel whose
 // waves share rows (24 rows of 128 dims over 3000 positions, 4 entries: 17.7
 // us, 18.5 by the other); more go to the one whose waves share keys, in tiles
-// of 128: two 2048-token chunks over 6000 positions 356 us, 497 in tiles of 64.
+// of 128: two 2048-token chunks 341 us, 497 in tiles of 64.
 // Tiles of 64 where the unit has no more, of 256 dims, whose sums take twice
 // the registers, and of 64 dims where they leave a quarter of the rows less
 // empty, which is from 129 to 192 rows.  Tiles of 64 and 128 there, us: 16 entries
