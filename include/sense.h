@@ -764,7 +764,9 @@ sense_status_t sense_kv_attention_workspace_size(const sense_kv_cache_t *cache, 
  * may overflow them.
  *   q, out      rows of n_heads x head_dim elements of q_dtype (F16, BF16),
  *               head h at h * head_dim; strides in elements; bases and strides
- *               multiples of 16 bytes.  out may be q.  Rows that the batch
+ *               multiples of 16 bytes.  out may be q where no row belongs to
+ *               two entries (one might find the other's result as its query),
+ *               and overlaps it in no other way.  Rows that the batch
  *               leaves out keep their contents.
  *   n_heads     a multiple of n_kv_heads, at most 4096.
  *   mask        uint8 (DEVICE) or NULL; mask_ld >= max_rows.

@@ -1138,7 +1138,8 @@ def sense_kv_attention(cache: dict, layer: int, q: torch.Tensor, mask: torch.Ten
     becomes 0.  ``max_kv`` bounds the sequences' lengths (0: the
     capacity); ``softmax_scale`` (in (0, 2^127]) is d**-0.5 by default.  Returns ``out``
     (like q; rows that belong to no entry keep what they hold, so without ``out``
-    they hold nothing in particular)."""
+    they hold nothing in particular; it may be q where no row belongs to two
+    entries)."""
     desc = _kv_desc(cache)
     dev = cache["codes"].device
     if q.dim() not in (3, 4) or q.dtype not in (torch.float16, torch.bfloat16) or q.device != dev:
